@@ -52,6 +52,9 @@ typedef enum { PO_SCHED_1F1B = 0, PO_SCHED_1F1B_INTERLEAVED = 1, PO_SCHED_GIS = 
  * chunks 0 .. ceil(r v) - 1 of every microbatch; equals ALTERNATE_MB if v == 1. */
 typedef enum { PO_SEL_ALTERNATE_MB = 0, PO_SEL_LONGEST_LIFESPAN = 1 } po_select;
 
+/* Which elements of a head a rotation takes as a pair: p and p + the number of pairs, or 2 p and 2 p + 1. */
+typedef enum { PO_ROTARY_HALVES = 0, PO_ROTARY_NEIGHBOURS = 1 } po_rotary_layout;
+
 typedef enum {
   PO_OK = 0,
   PO_E_INVAL = -1,      /* bad argument or unsupported shape */
@@ -311,6 +314,51 @@ int po_op_attention_forward(int32_t dtype, const void* qkv, void* o, float* lse,
 int po_op_attention_backward(int32_t dtype, const void* qkv, const void* o, const float* lse, const void* d_o,
                              void* dqkv, float* delta, void* partials, int32_t s, int32_t h, int32_t n_heads,
                              int32_t n_kv_heads, int32_t force_generic, void* stream);
+
+/* Packed sequences: n_sequences of them back to back in tensors of `rows` rows, of which the last may belong to none.
+ *
+ * The maps of such a batch, built on the GPU from its lengths (DEVICE int32 [n_sequences]), all int32 in DEVICE memory, any of them
+ * NULL if not wanted: starts [n_sequences + 1] (the first row of each and the row behind the last), positions [rows] (of a
+ * row in its sequence), sequence [rows] (whose row it is), the last two -1 behind the last sequence; and plan, po_op_packed_plan_bytes(rows) bytes, 16-byte
+ * aligned, which the attention calls below read: one plan serves every layer.  A length below zero counts as zero; sequences
+ * that reach past `rows` are cut there.  1 to 16384 sequences, 1 to 2097152 rows (beyond: PO_E_INVAL, and 0 bytes). */
+uint64_t po_op_packed_plan_bytes(int32_t rows);
+int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows, int32_t* starts, int32_t* positions,
+                      int32_t* sequence, void* plan, void* stream);
+
+/* Causal attention within each sequence of a packed batch: po_op_attention_forward and _backward for qkv [rows, h + 2 hkv], o and
+ * d_o [rows, h], lse [n_heads, rows], dqkv like qkv, head sizes 64 and 128, all tensors 16-byte aligned.  plan: as po_op_packed_plan left it
+ * for the same `rows` (of one made for another row count nothing is computed).  Rows behind the last sequence are not read as
+ * keys or queries and left as they were in every output.  An infinity or NaN in a row of one sequence reaches no other sequence,
+ * in a key or value row no row of o and dQ before it.  workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned,
+ * contents unspecified before and afterwards.  Results do not depend on how often or beside what a call runs: no atomics. */
+int po_op_attention_packed_forward(int32_t dtype, const void* qkv, const void* plan, void* o, float* lse, int32_t rows, int32_t h,
+                                   int32_t n_heads, int32_t n_kv_heads, void* stream);
+uint64_t po_op_attention_packed_backward_workspace(int32_t dtype, int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads);
+int po_op_attention_packed_backward(int32_t dtype, const void* qkv, const void* plan, const void* o, const float* lse, const void* d_o,
+                                    void* dqkv, void* workspace, int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads,
+                                    void* stream);
+
+/* Queries and keys normed head by head and rotated by their positions, from qkv [rows, h + 2 hkv] into out of the same shape; the
+ * values are copied (out may be qkv itself: they are then left alone).  Head size h / n_heads: a multiple of 16, at most 256.
+ * Norm: y = x / sqrt(mean(x^2) + eps) * gain over a head, gain_q [head size] for all query heads, gain_k for all key heads, both of
+ * dtype, both NULL: no norm.
+ * Rotation: pair p of a head (`layout`: a po_rotary_layout) turns by positions[axis, row] * inv_freq[p] radians, positions
+ * DEVICE int32 [n_axes, rows], n_axes 1 to 4, inv_freq DEVICE fp32; axis_pairs (HOST, [n_axes]) says how many pairs turn by each axis,
+ * the first axis_pairs[0] by axis 0 and so on.  Together they are a multiple of 8 and at most half the head size; elements
+ * behind them are not rotated.  Angles are formed in fp64.  A row whose position on axis 0 is negative holds nothing (positions of
+ * po_op_packed_plan behind the last sequence) and is left as it was in out.  All tensors 16-byte aligned. */
+int po_op_qk_norm_rotary_forward(int32_t dtype, const void* qkv, const void* gain_q, const void* gain_k, const int32_t* positions,
+                                 const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes, int32_t layout, void* out,
+                                 int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream);
+/* dqkv [rows, h + 2 hkv] = the gradient of qkv from that of out, d_out (dqkv may be d_out itself, not qkv); dgain_q, dgain_k [head
+ * size] fp32: += the gains' gradients, in a fixed order.  qkv is the input of the forward.  Without gains qkv, dgain_q, dgain_k and
+ * workspace may be NULL.  workspace: po_op_qk_norm_rotary_backward_workspace bytes, contents unspecified afterwards. */
+uint64_t po_op_qk_norm_rotary_backward_workspace(int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads);
+int po_op_qk_norm_rotary_backward(int32_t dtype, const void* d_out, const void* qkv, const void* gain_q, const void* gain_k,
+                                  const int32_t* positions, const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes,
+                                  int32_t layout, void* dqkv, float* dgain_q, float* dgain_k, float* workspace, int32_t rows,
+                                  int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream);
 
 /* out[r, c] = x[r, c] * keep(r, c) / (1 - p): one dropout site (site 0: after the attention output projection,
  * 1: after the MLP output projection) of global layer `layer` for microbatch `mb`.  keep(r, c) is true iff word

@@ -26,6 +26,7 @@ PO_F32, PO_BF16 = 0, 1
 PO_SCHED_1F1B, PO_SCHED_1F1B_INTERLEAVED, PO_SCHED_GIS, PO_SCHED_PO = 0, 1, 2, 3
 PO_SEL_ALTERNATE_MB, PO_SEL_LONGEST_LIFESPAN = 0, 1
 PO_OK, PO_E_INVAL, PO_E_STATE, PO_E_DEVICE_OOM, PO_E_HOST_OOM, PO_E_HIP = 0, -1, -2, -3, -4, -5
+PO_ROTARY_HALVES, PO_ROTARY_NEIGHBOURS = 0, 1
 OP_KINDS = ("F", "B", "OFFLOAD", "RELOAD", "W")
 
 
@@ -98,6 +99,17 @@ EXPORTS = {
     "po_op_gemm_tile": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
     "po_op_attention_forward": (C.c_int, [C.c_int32] + [C.c_void_p] * 3 + [C.c_int32] * 5 + [C.c_void_p]),
     "po_op_attention_backward": (C.c_int, [C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p]),
+    "po_op_packed_plan_bytes": (C.c_uint64, [C.c_int32]),
+    "po_op_packed_plan": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 5),
+    "po_op_attention_packed_forward": (C.c_int, [C.c_int32] + [C.c_void_p] * 4 + [C.c_int32] * 4 + [C.c_void_p]),
+    "po_op_attention_packed_backward_workspace": (C.c_uint64, [C.c_int32] * 5),
+    "po_op_attention_packed_backward": (C.c_int, [C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] * 4 + [C.c_void_p]),
+    "po_op_qk_norm_rotary_forward": (C.c_int, [C.c_int32] + [C.c_void_p] * 5 + [C.POINTER(C.c_int32), C.c_int32, C.c_int32,
+                                                                               C.c_void_p] + [C.c_int32] * 4 +
+                                     [C.c_float, C.c_void_p]),
+    "po_op_qk_norm_rotary_backward_workspace": (C.c_uint64, [C.c_int32] * 4),
+    "po_op_qk_norm_rotary_backward": (C.c_int, [C.c_int32] + [C.c_void_p] * 6 + [C.POINTER(C.c_int32), C.c_int32, C.c_int32] +
+                                      [C.c_void_p] * 4 + [C.c_int32] * 4 + [C.c_float, C.c_void_p]),
     "po_op_dropout": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_uint64,
                                 C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
     "po_set_dropout_seed": (C.c_int, [C.c_void_p, C.c_uint64]),
@@ -312,6 +324,50 @@ def po_op_attention_backward(dtype, qkv, o, lse, d_o, dqkv, delta, s, h, n_heads
                              n_kv_heads=0, partials=None):
     _check(lib.po_op_attention_backward(dtype, _ptr(qkv), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dqkv), _ptr(delta),
                                         _ptr(partials), s, h, n_heads, n_kv_heads, force_generic, _stream(stream)))
+
+
+def po_op_packed_plan_bytes(rows) -> int:
+    return lib.po_op_packed_plan_bytes(rows)
+
+
+def po_op_packed_plan(lengths, n_sequences, rows, starts=None, positions=None, sequence=None, plan=None, stream=None):
+    _check(lib.po_op_packed_plan(_ptr(lengths), n_sequences, rows, _ptr(starts), _ptr(positions), _ptr(sequence), _ptr(plan),
+                                 _stream(stream)))
+
+
+def po_op_attention_packed_forward(dtype, qkv, plan, o, lse, rows, h, n_heads, n_kv_heads=0, stream=None):
+    _check(lib.po_op_attention_packed_forward(dtype, _ptr(qkv), _ptr(plan), _ptr(o), _ptr(lse), rows, h, n_heads, n_kv_heads,
+                                              _stream(stream)))
+
+
+def po_op_attention_packed_backward_workspace(dtype, rows, h, n_heads, n_kv_heads=0) -> int:
+    return lib.po_op_attention_packed_backward_workspace(dtype, rows, h, n_heads, n_kv_heads)
+
+
+def po_op_attention_packed_backward(dtype, qkv, plan, o, lse, d_o, dqkv, workspace, rows, h, n_heads, n_kv_heads=0, stream=None):
+    _check(lib.po_op_attention_packed_backward(dtype, _ptr(qkv), _ptr(plan), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dqkv),
+                                               _ptr(workspace), rows, h, n_heads, n_kv_heads, _stream(stream)))
+
+
+def po_op_qk_norm_rotary_forward(dtype, qkv, gain_q, gain_k, positions, inv_freq, axis_pairs, layout, out, rows, h, n_heads,
+                                 n_kv_heads=0, eps=1e-6, stream=None):
+    """axis_pairs: list of how many pairs turn by each axis of positions [len(axis_pairs), rows]."""
+    _check(lib.po_op_qk_norm_rotary_forward(dtype, _ptr(qkv), _ptr(gain_q), _ptr(gain_k), _ptr(positions), _ptr(inv_freq),
+                                            (C.c_int32 * len(axis_pairs))(*axis_pairs), len(axis_pairs), layout, _ptr(out),
+                                            rows, h, n_heads, n_kv_heads, eps, _stream(stream)))
+
+
+def po_op_qk_norm_rotary_backward_workspace(rows, h, n_heads, n_kv_heads=0) -> int:
+    return lib.po_op_qk_norm_rotary_backward_workspace(rows, h, n_heads, n_kv_heads)
+
+
+def po_op_qk_norm_rotary_backward(dtype, d_out, qkv, gain_q, gain_k, positions, inv_freq, axis_pairs, layout, dqkv, dgain_q,
+                                  dgain_k, workspace, rows, h, n_heads, n_kv_heads=0, eps=1e-6, stream=None):
+    """axis_pairs: as for the forward."""
+    _check(lib.po_op_qk_norm_rotary_backward(dtype, _ptr(d_out), _ptr(qkv), _ptr(gain_q), _ptr(gain_k), _ptr(positions),
+                                             _ptr(inv_freq), (C.c_int32 * len(axis_pairs))(*axis_pairs), len(axis_pairs),
+                                             layout, _ptr(dqkv), _ptr(dgain_q), _ptr(dgain_k), _ptr(workspace), rows, h,
+                                             n_heads, n_kv_heads, eps, _stream(stream)))
 
 
 def po_op_dropout(dtype, x, out, rows, cols, p, seed, layer, site, mb, stream=None):

@@ -185,5 +185,46 @@ __device__ __forceinline__ void redo_dq_rows(uint32_t redo, int row0, const T* _
                                                      scale, dqkv + (size_t)i * ld + head * DH);
   }
 }
+// Key row j of dK and dV: dk_row[dh], dv_row[dh].  key(e) and value(e) are its elements, the key's scaled; `group` query heads read it, the
+// first at column 0 of q (rows ld apart) and d_o (rows h apart), row 0 of lse and delta (heads s apart); the last query row is `last`.
+template <typename T, int SLOTS, int AHEAD, typename Key, typename Value>
+__device__ __forceinline__ void attention_key_row(Key key, Value value, const T* __restrict__ q, const T* __restrict__ d_o, int ld,
+                                                  int h, const float* __restrict__ lse, const float* __restrict__ delta, int s,
+                                                  int group, int j, int last, int dh, int lane, float scale,
+                                                  T* __restrict__ dk_row, T* __restrict__ dv_row) {
+  float dk[SLOTS], dv[SLOTS];
+#pragma unroll
+  for (int r = 0; r < SLOTS; ++r) dk[r] = dv[r] = 0.f;
+  for (int g = 0; g < group; ++g)
+    for (int i0 = j; i0 <= last; i0 += kWave) {
+      const int i = i0 + lane, n = min(kWave, last - i0 + 1);
+      const T* q0 = q + (size_t)i0 * ld + g * dh;
+      const T* d0 = d_o + (size_t)i0 * h + g * dh;
+      float p = 0.f, ds = 0.f;
+      if (i <= last) {
+        const T* qr = q0 + (size_t)lane * ld;
+        const T* dr = d0 + (size_t)lane * h;
+        float sc = 0.f, dp = 0.f;
+        for (int e = 0; e < dh; e += AHEAD)
+#pragma unroll
+          for (int u = 0; u < AHEAD; ++u) {
+            sc = fmaf(key(e + u), to_f32(qr[e + u]), sc);
+            dp = fmaf(value(e + u), to_f32(dr[e + u]), dp);
+          }
+        p = __expf(sc - lse[(size_t)g * s + i]);
+        ds = p * (dp - delta[(size_t)g * s + i]);
+      }
+      accumulate_weighted_rows<T, SLOTS, AHEAD>(dv, p, d0, h, n, dh, lane);
+      accumulate_weighted_rows<T, SLOTS, AHEAD>(dk, ds, q0, ld, n, dh, lane);
+    }
+#pragma unroll
+  for (int r = 0; r < SLOTS; ++r) {
+    int e = lane + kWave * r;
+    if (e < dh) {
+      dk_row[e] = from_f32<T>(dk[r] * scale);
+      dv_row[e] = from_f32<T>(dv[r]);
+    }
+  }
+}
 
 }  // namespace po

@@ -163,6 +163,37 @@ bool attention_backward(int dtype, const void* qkv, const void* o, const float* 
                         float* delta, void* partials, int s, int h, int n_heads, int n_kv_heads, bool force_generic,
                         hipStream_t stream);
 
+// delta[head][row] = dO . O of that row and head, rows of h = n_heads * 64 or 128 elements (attention_mfma.hip).
+bool attention_delta_bf16(const bf16* o, const bf16* d_o, float* delta, int rows, int h, int n_heads, hipStream_t stream);
+
+// ---- packed sequences (packed_plan.hip, attention_packed.hip, attention_packed_f32.hip, qk_norm_rotary.hip) ------------
+size_t packed_plan_bytes(int rows);  // 0: too many rows
+bool packed_plan(const int* lengths, int n, int rows, int* starts, int* positions, int* sequence, int* plan,
+                 hipStream_t stream);
+// Causal attention within each sequence of the plan; head sizes 64 and 128, 16-byte aligned tensors.
+bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void* o, float* lse, int rows, int h, int n_heads,
+                              int n_kv_heads, hipStream_t stream);
+size_t attention_packed_backward_workspace(int dtype, int rows, int h, int n_heads, int n_kv_heads);
+bool attention_packed_backward(int dtype, const void* qkv, const int* plan, const void* o, const float* lse, const void* d_o,
+                               void* dqkv, void* workspace, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream);
+bool attention_packed_forward_f32(const float* qkv, const int* plan, float* o, float* lse, int rows, int h, int n_heads,
+                                  int n_kv_heads, hipStream_t stream);
+bool attention_packed_backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o,
+                                   float* dqkv, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream);
+constexpr int kMaxRotaryAxes = 4, kRotaryHalves = 0, kRotaryNeighbours = 1;
+struct QkNormRotary {
+  const void *gain_q, *gain_k;  // [head size] of dtype; both null: no norm
+  const int* positions;         // [n_axes, rows]; rows whose first is negative are left out
+  const float* inv_freq;        // [pairs]
+  const int* axis_pairs;        // HOST [n_axes]
+  int n_axes, layout, rows, h, n_heads, n_kv_heads;
+  float eps;
+};
+bool qk_norm_rotary_forward(int dtype, const QkNormRotary& a, const void* qkv, void* out, hipStream_t stream);
+size_t qk_norm_rotary_backward_workspace(int rows, int h, int n_heads);
+bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out, const void* qkv, void* dqkv, float* dgain_q,
+                             float* dgain_k, float* workspace, hipStream_t stream);
+
 #define PO_HIP_OK(expr)                                                                  \
   do {                                                                                   \
     hipError_t e__ = (expr);                                                             \

@@ -1,0 +1,345 @@
+// Queries and keys of a layer on their way from the projection to attention: every head normed by its root mean square and rotated by
+// its row's positions, one pass over q | k | v, forward and backward.
+//
+//   r = 1 / sqrt(mean(x^2) + eps), y = x r g (one gain for all query heads, one for all key heads; no norm: y = x)
+//   pair p = elements (a, b) of y, angle t = position[axis of p] inv_freq[p]:  (a cos t - b sin t, a sin t + b cos t)
+// backward, d the gradient of the output: u = the rotation by -t of d,
+//   dg += sum over rows and heads of u x r,  w = u g,  dx = r w - x (r^3 / head size) sum(w x)
+// Everything between the load and the one rounding of the store is fp32; angles are formed in fp64 and reduced to a turn there: in
+// fp32 position 10^6 would be a twentieth of a radian off.
+//
+// Bound by memory: each element is read and written once.  A wave takes a row at a time: lane p forms the cosine and sine of pair p once
+// for all heads, which read them back from LDS; then 64 / LANES heads at a time, a lane holding 16 elements (eight pairs) of one head.
+// The gains' gradients stay in registers over all rows of a wave, are added over the lanes and waves of a block in a fixed order, and a
+// second launch adds the blocks: no atomics.
+#include <algorithm>
+
+#include "kernels.h"
+
+namespace po {
+
+namespace {
+
+constexpr int kBlocks = 1024;  // of the backward at most: four on a CU; each leaves a partial sum of the gains' gradients
+constexpr int kMaxPairs = 128;
+
+struct Axes {
+  int end[kMaxRotaryAxes];  // the pairs [end[i - 1], end[i]) turn by axis i
+};
+
+// A lane's 16 elements of a head as eight pairs.  Halves: chunk l of the first half and of the second; behind the rotated part two chunks
+// in a row.  Neighbours: two chunks in a row.
+template <typename T>
+__device__ __forceinline__ void load8(float (&v)[8], const T* p) {
+  constexpr int V = Vec16<T>::N;
+#pragma unroll
+  for (int k = 0; k < 8; k += V) {
+    const Vec16<T> x = load16(p + k);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[k + i] = to_f32(x.v[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  constexpr int V = Vec16<T>::N;
+#pragma unroll
+  for (int k = 0; k < 8; k += V) {
+    Vec16<T> x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x.v[i] = from_f32<T>(v[k + i]);
+    store16(p + k, x);
+  }
+}
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ void load_pairs(float (&a)[8], float (&b)[8], const T* head, int at_a, int at_b) {
+  float x[8], y[8];
+  load8(x, head + at_a);
+  load8(y, head + at_b);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    a[i] = NEIGHBOURS ? (i < 4 ? x[2 * i] : y[2 * i - 8]) : x[i];
+    b[i] = NEIGHBOURS ? (i < 4 ? x[2 * i + 1] : y[2 * i - 7]) : y[i];
+  }
+}
+template <typename T, bool NEIGHBOURS>
+__device__ __forceinline__ void store_pairs(T* head, int at_a, int at_b, const float (&a)[8], const float (&b)[8]) {
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = NEIGHBOURS ? (i & 1 ? b[i / 2] : a[i / 2]) : a[i];
+    y[i] = NEIGHBOURS ? (i & 1 ? b[4 + i / 2] : a[4 + i / 2]) : b[i];
+  }
+  store8(head + at_a, x);
+  store8(head + at_b, y);
+}
+template <int LANES>
+__device__ __forceinline__ float sum_over_head(float v) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&sn)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = a[i] * c[i] - b[i] * sn[i];
+    b[i] = a[i] * sn[i] + b[i] * c[i];
+    a[i] = y;
+  }
+}
+// What the lanes of this wave left in LDS before is there for all of them after.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+struct Shape {
+  int rows, h, hkv, dh, pairs, n_heads, n_kv_heads;
+  float eps;
+};
+
+// BACKWARD: x_in is the input of the forward (null: no norm), in the gradient of its output, out that of its input.
+template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD>
+__global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const T* __restrict__ x_in, const T* __restrict__ gain_q,
+                                                             const T* __restrict__ gain_k, const int* __restrict__ positions,
+                                                             const float* __restrict__ inv_freq, Axes axes, T* out,
+                                                             float* __restrict__ partials, Shape s) {
+  __shared__ float2 turns[4][kMaxPairs];
+  __shared__ float sums[BACKWARD ? 4 : 1][BACKWARD ? 2 * 16 * LANES : 1];
+  constexpr int HEADS = 64 / LANES;  // of a wave at a time
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (LANES - 1);
+  const int ld = s.h + 2 * s.hkv, heads = s.n_heads + s.n_kv_heads;
+  const bool held = 16 * l < s.dh, rotated = 8 * l < s.pairs, norm = gain_q != nullptr;
+  const int at_a = NEIGHBOURS || !rotated ? 16 * l : 8 * l, at_b = NEIGHBOURS || !rotated ? 16 * l + 8 : s.pairs + 8 * l;
+  float gq_a[8], gq_b[8], gk_a[8], gk_b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) gq_a[i] = gq_b[i] = gk_a[i] = gk_b[i] = 1.f;
+  if (norm && held) {
+    load_pairs<T, NEIGHBOURS>(gq_a, gq_b, gain_q, at_a, at_b);
+    load_pairs<T, NEIGHBOURS>(gk_a, gk_b, gain_k, at_a, at_b);
+  }
+  float dq_a[8], dq_b[8], dk_a[8], dk_b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) dq_a[i] = dq_b[i] = dk_a[i] = dk_b[i] = 0.f;
+
+  for (int row = blockIdx.x * 4 + wave; row < s.rows; row += gridDim.x * 4) {
+    if (positions[row] < 0) continue;  // no token there
+    for (int p = lane; p < s.pairs; p += 64) {
+      int axis = 0;
+#pragma unroll
+      for (int i = 0; i + 1 < kMaxRotaryAxes; ++i) axis += p >= axes.end[i];
+      const double turn = (double)positions[(size_t)axis * s.rows + row] * (double)inv_freq[p] * 0.15915494309189533577;
+      float2 cs;
+      sincospif(2.f * (float)(turn - rint(turn)), &cs.y, &cs.x);
+      turns[wave][p] = cs;
+    }
+    wave_sync();
+    float c[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 cs = rotated ? turns[wave][8 * l + i] : make_float2(1.f, 0.f);
+      c[i] = cs.x;
+      sn[i] = BACKWARD ? -cs.y : cs.y;
+    }
+    wave_sync();
+    for (int head0 = 0; head0 < heads; head0 += HEADS) {
+      const int head = head0 + lane / LANES;
+      const bool mine = held && head < heads, is_q = head < s.n_heads;
+      const size_t at = (size_t)row * ld + (size_t)head * s.dh;
+      float a[8], b[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
+      if (mine) load_pairs<T, NEIGHBOURS>(a, b, in + at, at_a, at_b);
+      if constexpr (!BACKWARD) {
+        if (norm) {
+          float sq = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sq = fmaf(a[i], a[i], fmaf(b[i], b[i], sq));
+          const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            a[i] *= r * (is_q ? gq_a[i] : gk_a[i]);
+            b[i] *= r * (is_q ? gq_b[i] : gk_b[i]);
+          }
+        }
+        if (rotated) rotate(a, b, c, sn);
+      } else {
+        if (rotated) rotate(a, b, c, sn);
+        if (norm) {
+          float x[8], y[8], sq = 0.f, dot = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
+          if (mine) load_pairs<T, NEIGHBOURS>(x, y, x_in + at, at_a, at_b);
+          float w[8], z[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            w[i] = a[i] * (is_q ? gq_a[i] : gk_a[i]);
+            z[i] = b[i] * (is_q ? gq_b[i] : gk_b[i]);
+            sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+            dot = fmaf(w[i], x[i], fmaf(z[i], y[i], dot));
+          }
+          const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
+          const float f = r * r * r * (sum_over_head<LANES>(dot) / (float)s.dh);
+          const float rq = is_q ? r : 0.f, rk = is_q ? 0.f : r;
+          if (mine) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float ta = a[i] * x[i], tb = b[i] * y[i];
+              dq_a[i] = fmaf(ta, rq, dq_a[i]);
+              dq_b[i] = fmaf(tb, rq, dq_b[i]);
+              dk_a[i] = fmaf(ta, rk, dk_a[i]);
+              dk_b[i] = fmaf(tb, rk, dk_b[i]);
+              a[i] = r * w[i] - x[i] * f;
+              b[i] = r * z[i] - y[i] * f;
+            }
+          }
+        }
+      }
+      if (mine) store_pairs<T, NEIGHBOURS>(out + at, at_a, at_b, a, b);
+    }
+    if (in != out) {  // the values pass
+      constexpr int V = Vec16<T>::N;
+      const size_t v0 = (size_t)row * ld + s.h + s.hkv;
+      for (int e = lane * V; e < s.hkv; e += 64 * V) store16(out + v0 + e, load16(in + v0 + e));
+    }
+  }
+  if constexpr (BACKWARD) {
+    if (!norm) return;
+    // element order of the gain: what a lane's pair i is at
+    float* mine = sums[wave];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[4] = {dq_a[i], dq_b[i], dk_a[i], dk_b[i]};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int o = LANES; o < 64; o <<= 1) v[k] += __shfl_xor(v[k], o, 64);
+      if (lane < LANES && held) {
+        const int ea = NEIGHBOURS ? 16 * l + 2 * i : at_a + i, eb = NEIGHBOURS ? 16 * l + 2 * i + 1 : at_b + i;
+        mine[ea] = v[0];
+        mine[eb] = v[1];
+        mine[s.dh + ea] = v[2];
+        mine[s.dh + eb] = v[3];
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * s.dh; e += 256)
+      partials[(size_t)blockIdx.x * 2 * s.dh + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+  }
+}
+
+// dgain_q, dgain_k [dh] += the blocks' partial sums [blocks][2 dh]: a block 16 columns, a thread every sixteenth row of one.
+__global__ __launch_bounds__(256) void rotary_gain_sum_kernel(const float* __restrict__ partials, int blocks, int dh,
+                                                              float* __restrict__ dgain_q, float* __restrict__ dgain_k) {
+  __shared__ float sums[16][17];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, e = blockIdx.x * 16 + x;
+  float v = 0.f;
+  if (e < 2 * dh)
+    for (int b = y; b < blocks; b += 16) v += partials[(size_t)b * 2 * dh + e];
+  sums[y][x] = v;
+  __syncthreads();
+  if (y || e >= 2 * dh) return;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < 16; k += 2 * o) sums[k][x] += sums[k + o][x];
+  float* to = e < dh ? dgain_q + e : dgain_k + (e - dh);
+  *to += sums[0][x];
+}
+
+bool check(const char* what, const QkNormRotary& a, const void* in, const void* x_in, const void* out, Axes& axes, Shape& s) {
+  const int dh = a.n_heads > 0 ? a.h / a.n_heads : 0;
+  if (a.rows <= 0 || a.h <= 0 || a.n_heads <= 0 || a.h % a.n_heads != 0 || a.n_kv_heads <= 0 || a.n_heads % a.n_kv_heads != 0 ||
+      dh % 16 != 0 || dh < 16 || dh > 256) {
+    set_error("%s: rows=%d h=%d heads=%d kv_heads=%d (head size h / heads a multiple of 16 up to 256, kv_heads a divisor of heads)",
+              what, a.rows, a.h, a.n_heads, a.n_kv_heads);
+    return false;
+  }
+  if ((int64_t)a.h + 2 * (int64_t)a.n_kv_heads * dh > INT32_MAX) {
+    set_error("%s: a row of h=%d and %d key/value heads is too long", what, a.h, a.n_kv_heads);
+    return false;
+  }
+  if (a.n_axes < 1 || a.n_axes > kMaxRotaryAxes || !a.axis_pairs) {
+    set_error("%s: n_axes=%d axis_pairs=%p (1 to %d axes)", what, a.n_axes, (const void*)a.axis_pairs, kMaxRotaryAxes);
+    return false;
+  }
+  int64_t pairs = 0;
+  for (int i = 0; i < kMaxRotaryAxes; ++i) {
+    if (i < a.n_axes && a.axis_pairs[i] < 0) pairs = -1;
+    if (i < a.n_axes && pairs >= 0) pairs += a.axis_pairs[i];
+    axes.end[i] = i + 1 < a.n_axes ? (int)std::min<int64_t>(pairs, INT32_MAX) : INT32_MAX;
+    if (pairs < 0) break;
+  }
+  if (pairs < 0 || pairs > dh / 2 || pairs % 8 != 0 || (a.layout != kRotaryHalves && a.layout != kRotaryNeighbours)) {
+    set_error("%s: %lld pairs of heads of %d, layout %d (pairs per axis not negative, together a multiple of 8 and at most half the "
+              "head size; layout 0 or 1)", what, (long long)pairs, dh, a.layout);
+    return false;
+  }
+  if (!(a.eps >= 0.f) || a.eps > 3e38f || (a.gain_q == nullptr) != (a.gain_k == nullptr)) {
+    set_error("%s: eps=%g gain_q=%p gain_k=%p (eps finite and not negative, both gains or none)", what, a.eps, a.gain_q, a.gain_k);
+    return false;
+  }
+  if (!in || !out || !a.positions || (pairs > 0 && !a.inv_freq) ||
+      ((uintptr_t)in | (uintptr_t)x_in | (uintptr_t)out | (uintptr_t)a.gain_q | (uintptr_t)a.gain_k) % 16 != 0 ||
+      ((uintptr_t)a.positions | (uintptr_t)a.inv_freq) % 4 != 0) {
+    set_error("%s: a NULL pointer, or one that is not 16-byte aligned", what);
+    return false;
+  }
+  s = Shape{a.rows, a.h, a.n_kv_heads * dh, dh, (int)pairs, a.n_heads, a.n_kv_heads, a.eps};
+  return true;
+}
+
+template <typename T, int LANES, bool BACKWARD>
+void launch(const QkNormRotary& a, const void* in, const void* x_in, void* out, float* partials, const Axes& axes, const Shape& s,
+            int blocks, hipStream_t stream) {
+  auto k = a.layout == kRotaryNeighbours ? qk_norm_rotary_kernel<T, LANES, true, BACKWARD> : qk_norm_rotary_kernel<T, LANES, false, BACKWARD>;
+  k<<<blocks, 256, 0, stream>>>((const T*)in, (const T*)x_in, (const T*)a.gain_q, (const T*)a.gain_k, a.positions, a.inv_freq, axes,
+                                (T*)out, partials, s);
+}
+template <bool BACKWARD>
+void launch(int dtype, const QkNormRotary& a, const void* in, const void* x_in, void* out, float* partials, const Axes& axes,
+            const Shape& s, int blocks, hipStream_t stream) {
+  auto k = s.dh <= 32    ? (dtype == kF32 ? launch<float, 2, BACKWARD> : launch<bf16, 2, BACKWARD>)
+           : s.dh <= 64  ? (dtype == kF32 ? launch<float, 4, BACKWARD> : launch<bf16, 4, BACKWARD>)
+           : s.dh <= 128 ? (dtype == kF32 ? launch<float, 8, BACKWARD> : launch<bf16, 8, BACKWARD>)
+                         : (dtype == kF32 ? launch<float, 16, BACKWARD> : launch<bf16, 16, BACKWARD>);
+  k(a, in, x_in, out, partials, axes, s, blocks, stream);
+}
+int backward_blocks(int rows) { return std::min(ceil_div(rows, 4), kBlocks); }
+
+}  // namespace
+
+size_t qk_norm_rotary_backward_workspace(int rows, int h, int n_heads) {
+  return (size_t)backward_blocks(rows) * 2 * (h / n_heads) * sizeof(float);
+}
+
+bool qk_norm_rotary_forward(int dtype, const QkNormRotary& a, const void* qkv, void* out, hipStream_t stream) {
+  Axes axes;
+  Shape s;
+  if (!check("qk_norm_rotary_forward", a, qkv, nullptr, out, axes, s)) return false;
+  launch<false>(dtype, a, qkv, nullptr, out, nullptr, axes, s, ceil_div(a.rows, 4), stream);
+  return launch_ok("qk_norm_rotary_kernel");
+}
+
+bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out, const void* qkv, void* dqkv, float* dgain_q,
+                             float* dgain_k, float* workspace, hipStream_t stream) {
+  Axes axes;
+  Shape s;
+  if (!check("qk_norm_rotary_backward", a, d_out, qkv, dqkv, axes, s)) return false;
+  if (a.gain_q && (!qkv || !dgain_q || !dgain_k || !workspace || ((uintptr_t)dgain_q | (uintptr_t)dgain_k | (uintptr_t)workspace) % 4 != 0)) {
+    set_error("qk_norm_rotary_backward: with gains, qkv=%p dgain_q=%p dgain_k=%p and workspace=%p are needed", qkv, (void*)dgain_q,
+              (void*)dgain_k, (void*)workspace);
+    return false;
+  }
+  if (qkv == dqkv && a.gain_q) {
+    set_error("qk_norm_rotary_backward: dqkv may be d_out, but not qkv");
+    return false;
+  }
+  const int blocks = backward_blocks(a.rows);
+  launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, blocks, stream);
+  if (a.gain_q) rotary_gain_sum_kernel<<<ceil_div(2 * s.dh, 16), 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
+  return launch_ok("qk_norm_rotary_kernel");
+}
+
+}  // namespace po

@@ -1891,6 +1891,54 @@ int po_op_attention_backward(int32_t dtype, const void* qkv, const void* o, cons
   return ok(attention_backward(dtype, qkv, o, lse, d_o, dqkv, delta, partials, s, h, n_heads,
                                n_kv_heads > 0 ? n_kv_heads : n_heads, force_generic != 0, (hipStream_t)stream));
 }
+uint64_t po_op_packed_plan_bytes(int32_t rows) { return packed_plan_bytes(rows); }
+int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows, int32_t* starts, int32_t* positions,
+                      int32_t* sequence, void* plan, void* stream) {
+  begin_launch();
+  return ok(packed_plan(lengths, n_sequences, rows, starts, positions, sequence, (int*)plan, (hipStream_t)stream));
+}
+int po_op_attention_packed_forward(int32_t dtype, const void* qkv, const void* plan, void* o, float* lse, int32_t rows, int32_t h,
+                                   int32_t n_heads, int32_t n_kv_heads, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(attention_packed_forward(dtype, qkv, (const int*)plan, o, lse, rows, h, n_heads, n_kv_heads > 0 ? n_kv_heads : n_heads,
+                                     (hipStream_t)stream));
+}
+uint64_t po_op_attention_packed_backward_workspace(int32_t dtype, int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads) {
+  if ((dtype != PO_F32 && dtype != PO_BF16) || rows <= 0 || h <= 0 || n_heads <= 0) return 0;
+  return attention_packed_backward_workspace(dtype, rows, h, n_heads, n_kv_heads > 0 ? n_kv_heads : n_heads);
+}
+int po_op_attention_packed_backward(int32_t dtype, const void* qkv, const void* plan, const void* o, const float* lse, const void* d_o,
+                                    void* dqkv, void* workspace, int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads,
+                                    void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(attention_packed_backward(dtype, qkv, (const int*)plan, o, lse, d_o, dqkv, workspace, rows, h, n_heads,
+                                      n_kv_heads > 0 ? n_kv_heads : n_heads, (hipStream_t)stream));
+}
+int po_op_qk_norm_rotary_forward(int32_t dtype, const void* qkv, const void* gain_q, const void* gain_k, const int32_t* positions,
+                                 const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes, int32_t layout, void* out,
+                                 int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  const QkNormRotary a{gain_q, gain_k, positions, inv_freq, axis_pairs, n_axes, layout, rows, h, n_heads,
+                       n_kv_heads > 0 ? n_kv_heads : n_heads, eps};
+  return ok(qk_norm_rotary_forward(dtype, a, qkv, out, (hipStream_t)stream));
+}
+uint64_t po_op_qk_norm_rotary_backward_workspace(int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads) {
+  (void)n_kv_heads;
+  return rows > 0 && h > 0 && n_heads > 0 ? qk_norm_rotary_backward_workspace(rows, h, n_heads) : 0;
+}
+int po_op_qk_norm_rotary_backward(int32_t dtype, const void* d_out, const void* qkv, const void* gain_q, const void* gain_k,
+                                  const int32_t* positions, const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes,
+                                  int32_t layout, void* dqkv, float* dgain_q, float* dgain_k, float* workspace, int32_t rows,
+                                  int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  const QkNormRotary a{gain_q, gain_k, positions, inv_freq, axis_pairs, n_axes, layout, rows, h, n_heads,
+                       n_kv_heads > 0 ? n_kv_heads : n_heads, eps};
+  return ok(qk_norm_rotary_backward(dtype, a, d_out, qkv, dqkv, dgain_q, dgain_k, workspace, (hipStream_t)stream));
+}
 int po_op_dropout(int32_t dtype, const void* x, void* out, int32_t rows, int32_t cols, float p, uint64_t seed,
                   int32_t layer, int32_t site, int32_t mb, void* stream) {
   begin_launch();
