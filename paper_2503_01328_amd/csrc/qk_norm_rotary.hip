@@ -106,18 +106,24 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
                                                              const float* __restrict__ inv_freq, Axes axes, T* out,
                                                              float* __restrict__ partials, Shape s) {
   __shared__ float2 turns[4][kMaxPairs];
+  __shared__ __align__(16) float gains[2 * LANES][16];  // for queries, for keys
   __shared__ float sums[BACKWARD ? 4 : 1][BACKWARD ? 2 * 16 * LANES : 1];
   constexpr int HEADS = 64 / LANES;  // of a wave at a time
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (LANES - 1);
   const int ld = s.h + 2 * s.hkv, heads = s.n_heads + s.n_kv_heads;
   const bool held = 16 * l < s.dh, rotated = 8 * l < s.pairs, norm = gain_q != nullptr;
   const int at_a = NEIGHBOURS || !rotated ? 16 * l : 8 * l, at_b = NEIGHBOURS || !rotated ? 16 * l + 8 : s.pairs + 8 * l;
-  float gq_a[8], gq_b[8], gk_a[8], gk_b[8];
+  if (norm) {  // a lane's sixteen gains next to each other
+    if (threadIdx.x < 2 * LANES) {
+      float a[8] = {}, b[8] = {};  // lanes without elements add zeros to a head's sums
+      if (held) load_pairs<T, NEIGHBOURS>(a, b, threadIdx.x < LANES ? gain_q : gain_k, at_a, at_b);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) gq_a[i] = gq_b[i] = gk_a[i] = gk_b[i] = 1.f;
-  if (norm && held) {
-    load_pairs<T, NEIGHBOURS>(gq_a, gq_b, gain_q, at_a, at_b);
-    load_pairs<T, NEIGHBOURS>(gk_a, gk_b, gain_k, at_a, at_b);
+      for (int i = 0; i < 8; ++i) {
+        gains[threadIdx.x][i] = a[i];
+        gains[threadIdx.x][8 + i] = b[i];
+      }
+    }
+    __syncthreads();
   }
   float dq_a[8], dq_b[8], dk_a[8], dk_b[8];
 #pragma unroll
@@ -147,6 +153,7 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
       const int head = head0 + lane / LANES;
       const bool mine = held && head < heads, is_q = head < s.n_heads;
       const size_t at = (size_t)row * ld + (size_t)head * s.dh;
+      const float* gain = gains[(is_q ? 0 : LANES) + l];
       float a[8], b[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
@@ -159,8 +166,8 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
           const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            a[i] *= r * (is_q ? gq_a[i] : gk_a[i]);
-            b[i] *= r * (is_q ? gq_b[i] : gk_b[i]);
+            a[i] *= r * gain[i];
+            b[i] *= r * gain[8 + i];
           }
         }
         if (rotated) rotate(a, b, c, sn);
@@ -174,8 +181,8 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
           float w[8], z[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            w[i] = a[i] * (is_q ? gq_a[i] : gk_a[i]);
-            z[i] = b[i] * (is_q ? gq_b[i] : gk_b[i]);
+            w[i] = a[i] * gain[i];
+            z[i] = b[i] * gain[8 + i];
             sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
             dot = fmaf(w[i], x[i], fmaf(z[i], y[i], dot));
           }
@@ -229,21 +236,28 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
   }
 }
 
-// dgain_q, dgain_k [dh] += the blocks' partial sums [blocks][2 dh]: a block 16 columns, a thread every sixteenth row of one.
+// dgain_q, dgain_k [dh] += the blocks' partial sums [blocks][2 dh]: a block eight columns, a thread every 32nd row of one (sixteen columns and every
+// sixteenth row took 25 us for 1024 rows, a load at a time).
 __global__ __launch_bounds__(256) void rotary_gain_sum_kernel(const float* __restrict__ partials, int blocks, int dh,
                                                               float* __restrict__ dgain_q, float* __restrict__ dgain_k) {
-  __shared__ float sums[16][17];
-  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, e = blockIdx.x * 16 + x;
+  __shared__ float sums[32][9];
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, e = blockIdx.x * 8 + x;  // 2 dh is a multiple of 8
+  const float* p = partials + e;
   float v = 0.f;
-  if (e < 2 * dh)
-    for (int b = y; b < blocks; b += 16) v += partials[(size_t)b * 2 * dh + e];
+  for (int b = y; b < blocks; b += 32 * 8) {
+    float u[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] = b + 32 * k < blocks ? p[(size_t)(b + 32 * k) * 2 * dh] : 0.f;
+    v += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
+  }
   sums[y][x] = v;
   __syncthreads();
-  if (y || e >= 2 * dh) return;
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-    for (int k = 0; k < 16; k += 2 * o) sums[k][x] += sums[k + o][x];
+  for (int o = 16; o > 0; o >>= 1) {
+    if (y < o) sums[y][x] += sums[y + o][x];
+    __syncthreads();
+  }
+  if (y) return;
   float* to = e < dh ? dgain_q + e : dgain_k + (e - dh);
   *to += sums[0][x];
 }
@@ -338,7 +352,7 @@ bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out
   }
   const int blocks = backward_blocks(a.rows);
   launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, blocks, stream);
-  if (a.gain_q) rotary_gain_sum_kernel<<<ceil_div(2 * s.dh, 16), 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
+  if (a.gain_q) rotary_gain_sum_kernel<<<2 * s.dh / 8, 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
   return launch_ok("qk_norm_rotary_kernel");
 }
 
