@@ -1513,15 +1513,6 @@ __global__ __launch_bounds__(256) void attn_delta_mfma_path_kernel(const bf16* _
 // ==================================================================================
 // Host side
 // ==================================================================================
-bool attention_delta_bf16(const bf16* o, const bf16* d_o, float* delta, int rows, int h, int n_heads, hipStream_t stream) {
-  const unsigned blocks = (unsigned)(((size_t)rows * h / 8 + 255) / 256);
-  if (h / n_heads == 128)
-    attn_delta_mfma_path_kernel<128><<<blocks, 256, 0, stream>>>(o, d_o, delta, rows, h);
-  else
-    attn_delta_mfma_path_kernel<64><<<blocks, 256, 0, stream>>>(o, d_o, delta, rows, h);
-  return launch_ok("attn_delta_mfma_path_kernel");
-}
-
 bool attention_mfma_supported(int s, int h, int n_heads, int n_kv_heads) {
   if (n_heads <= 0 || h % n_heads != 0 || n_kv_heads <= 0 || n_heads % n_kv_heads != 0) return false;
   if (s % 128 != 0 && s > 128 * kMaxGridY) return false;

@@ -10,10 +10,26 @@
 // accumulators are fp32.
 // A key or value that is not finite reaches the rows that see it and no other, nor does a row of d_o reach another sequence: results that
 // are not finite are redone row by row (attention_packed_rows.h).  Rows behind the last sequence read as zeros and are never written.
+#include <algorithm>
+
 #include "attention_few_tile.h"
 #include "attention_packed_rows.h"
 
 namespace po {
+template <int BEGIN, int END, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (BEGIN < END) {
+    f(std::integral_constant<int, BEGIN>());
+    static_for<BEGIN + 1, END>(f);
+  }
+}
+
+// Waits for all loads in a way that the compiler sees.  It counts the loads of its own that may be outstanding (a kernel's rows, read into registers), cannot
+// see those requested by text, and would guard every use of such a register in the loop with a wait that is really one for the tiles under way.
+__device__ __forceinline__ void wait_loads_visibly() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), the other counters left alone (expcnt 7, lgkmcnt 15)
+  asm volatile("" ::: "memory");
+}
 
 template <int DH>
 __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel(const bf16* __restrict__ qkv, const int* words,
@@ -27,7 +43,7 @@ __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int n_heads = h / DH, head = blockIdx.x % n_heads, at = blockIdx.x / n_heads;
   if (total == 0) return;
-  const int q0 = plan.key_order()[at >> 2] * kPlanBlock + (3 - (at & 3)) * kRows;
+  const int q0 = plan.key_order()[at >> 2].x * kPlanBlock + (3 - (at & 3)) * kRows;
   if (q0 >= total) return;
   const int q = q0 + (lane & 31), ld = h + 2 * hkv, last = total - 1;
   const int first = plan.first()[q], first_lo = plan.first()[q0], first_hi = plan.first()[min(q0 + kRows - 1, last)];
@@ -47,6 +63,7 @@ __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel
     if (t0 + wave + i * W < t_end) request(i, t0 + wave + i * W);
   bf16x8 qf[DH / 16];
   load_row<DH>(qf, qkv + (size_t)min(q, last) * ld + head * DH, half);  // (rows past the end: computed, not stored)
+  wait_loads_visibly();
   f32x16 acc[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) acc[d] = zero16();
@@ -121,33 +138,35 @@ __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel
     l += stat[(W + w) * 64 + lane] * f[w];
   }
   const uint32_t redo = all_redo<W>(redo_of) & rows_to_redo(!is_nan(l), 32);
-  if (redo) redo_packed_forward_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, o, lse, h, hkv, group, head, scale);
-  if (q > last || (redo >> (lane & 31) & 1)) return;
-  const float inv = 1.0f / l;
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
+    const float inv = 1.0f / l;
 #pragma unroll
-  for (int g = wave; g < 4 * DT; g += W) {
-    f32x4 v;
+    for (int g = wave; g < 4 * DT; g += W) {
+      f32x4 v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f;
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) x += part[w * PART + (4 * g + r) * 64 + lane] * f[w];
-      v[r] = x * inv;
+        for (int w = 0; w < W; ++w) x += part[w * PART + (4 * g + r) * 64 + lane] * f[w];
+        v[r] = x * inv;
+      }
+      store4(o + (size_t)q * h + head * DH + 8 * g + 4 * half, v);
     }
-    store4(o + (size_t)q * h + head * DH + 8 * g + 4 * half, v);
   }
-  if (wave == 0 && half == 0) {
+  if (wave == 0 && half == 0 && q <= last) {
     // by whichever constant is the more exact: 1 / 8, or c ln 2, whose two roundings all but cancel
     const float log_l = __logf(l), ln2 = 0.6931471805599453f;
     lse[(size_t)head * rows + q] = DH == 64 ? m * scale + fmaf(fmaf(-m, c, mc), ln2, log_l) : fmaf(mc, ln2, log_l);
   }
+  if (redo) redo_packed_forward_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, o, h, hkv, group, head, scale);
 }
 
 // 32 query rows of a head from q0 on.
 template <int DH>
 __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head, PackedPlan plan, int total,
                                                     const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                    const float* __restrict__ lse, const float* __restrict__ delta,
+                                                    const float* __restrict__ lse,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
                                                     bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
   using F = Few<DH>;
   constexpr int DT = DH / 32, W = F::W, PART = F::NS * F::STAGE / 4;
@@ -171,7 +190,8 @@ __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head
   bf16x8 qf[DH / 16], dof[DH / 16];
   load_row<DH>(qf, qkv + (size_t)qc * ld + head * DH, half);
   load_row<DH>(dof, d_o + (size_t)qc * h + head * DH, half);
-  const float lse_q = lse[(size_t)head * plan.rows + qc] * kLog2e, delta_q = delta[(size_t)head * plan.rows + qc];
+  const float lse_q = from_lse[(size_t)head * plan.rows + qc] * -c, delta_q = -from_delta[(size_t)head * plan.rows + qc];
+  wait_loads_visibly();
   f32x16 dq[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) dq[d] = zero16();
@@ -204,27 +224,29 @@ __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head
   if (lane == 0) redo_of[wave] = mine;
   __syncthreads();
   const uint32_t redo = all_redo<W>(redo_of);
-  if (redo) redo_packed_dq_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, d_o, lse, delta, dqkv, h, hkv, group, head, scale);
-  if (q > last || (redo >> (lane & 31) & 1)) return;
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
 #pragma unroll
-  for (int g = wave; g < 4 * DT; g += W) {
-    f32x4 v;
+    for (int g = wave; g < 4 * DT; g += W) {
+      f32x4 v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f;
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) x += part[w * PART + (4 * g + r) * 64 + lane];
-      v[r] = x * scale;
+        for (int w = 0; w < W; ++w) x += part[w * PART + (4 * g + r) * 64 + lane];
+        v[r] = x * scale;
+      }
+      store4(dqkv + (size_t)q * ld + head * DH + 8 * g + 4 * half, v);
     }
-    store4(dqkv + (size_t)q * ld + head * DH + 8 * g + 4 * half, v);
   }
+  if (redo) redo_packed_dq_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
 }
 
 // 32 keys of a key/value head from k0 on; its waves walk the query tiles of every query head that reads it.
 template <int DH>
 __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_head, PackedPlan plan, int total,
                                                      const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                     const float* __restrict__ lse, const float* __restrict__ delta,
+                                                     const float* __restrict__ lse,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
                                                      bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
   using F = Few<DH>;
   constexpr int DT = DH / 32, W = F::W, PART = F::NS * F::STAGE / 4;
@@ -232,13 +254,13 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
   const int key = k0 + (lane & 31), ld = h + 2 * hkv, last = total - 1, head0 = kv_head * group;
   const int end = plan.end()[key], end_lo = plan.end()[k0], end_hi = plan.end()[min(k0 + kRows - 1, last)];
   const int t0 = k0 / kRows, n_q = (end_hi - 1) / kRows + 1 - t0, n_it = group * n_q;
-  const float c = scale * kLog2e, from_lse = -1.0f / scale;
+  const float c = scale * kLog2e;
   char* stages = smem + wave * F::NS * F::STAGE;
-  char* stats = smem + F::AFTER + wave * F::NS * 256;  // per stage lse and delta of the tile's 32 rows
+  char* stats = smem + F::AFTER + wave * F::NS * 256;  // per stage the statistics of the tile's 32 rows
   const unsigned stages_lds = __builtin_amdgcn_readfirstlane((int)lds_byte(stages));
   const unsigned stats_lds = __builtin_amdgcn_readfirstlane((int)lds_byte(stats));
   const TileLoads<DH> q_loads(ld, lane), do_loads(h, lane);
-  const float* stat_of = half ? delta : lse;
+  const float* stat_of = half ? from_delta : from_lse;
   auto request = [&](int i, int it) {
     const int g = it / n_q, q0 = (t0 + it - g * n_q) * kRows, head = head0 + g;
     q_loads.request(stages_lds + i % F::NS * F::STAGE, qkv + head * DH, ld, q0, total);
@@ -252,6 +274,7 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
   const bf16* krow = qkv + (size_t)min(key, last) * ld + h + kv_head * DH;  // (keys past the end: computed, not stored)
   load_row<DH>(kf, krow, half);
   load_row<DH>(vf, krow + hkv, half);
+  wait_loads_visibly();
   f32x16 dk[DT], dv[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) dk[d] = dv[d] = zero16();
@@ -268,8 +291,8 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
       const f32x4 vd = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * b + 4 * half);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[4 * b + r] = vl[r] * from_lse;
-        ds[4 * b + r] = -vd[r];
+        p[4 * b + r] = vl[r];
+        ds[4 * b + r] = vd[r];
       }
     }
     p = dot_tile<DH>(qtile, kf, p, lane);
@@ -295,39 +318,41 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
   put_partial<DT>(part + wave * PART, dk, lane);
   put_partial<DT>(part + wave * PART + PART / 2, dv, lane);
   uint32_t* redo_of = reinterpret_cast<uint32_t*>(smem + F::AFTER + W * F::NS * 256);
-  const uint32_t mine = rows_to_redo(not_finite<DT>(dk) || not_finite<DT>(dv), total - k0);
-  if (lane == 0) redo_of[wave] = mine;
+  const uint32_t bad_k = rows_to_redo(not_finite<DT>(dk), total - k0), bad_v = rows_to_redo(not_finite<DT>(dv), total - k0);
+  if (lane == 0) redo_of[wave] = bad_k, redo_of[W + wave] = bad_v;
   __syncthreads();
   bf16* out = dqkv + h + kv_head * DH;
-  const uint32_t redo = all_redo<W>(redo_of);
-  if (redo)
-    redo_packed_key_rows<bf16, DH>(share_of<W>(redo, wave), k0, plan, qkv, d_o, lse, delta, out, out + hkv, ld, h, hkv, group, group,
-                                   head0, scale);
-  if (key > last || (redo >> (lane & 31) & 1)) return;
-  out += (size_t)key * ld + 4 * half;
+  const size_t stat_at = (size_t)head0 * plan.rows;
+  const uint32_t redo = keys_to_redo(all_redo<W>(redo_of), all_redo<W>(redo_of + W), lse + stat_at, from_delta + stat_at, min(key, last), group, plan.rows);
+  if (key <= last && !(redo >> (lane & 31) & 1)) {
+    bf16* to = out + (size_t)key * ld + 4 * half;
 #pragma unroll
-  for (int g = wave; g < 4 * DT; g += W) {
-    f32x4 vk, vv;
+    for (int g = wave; g < 4 * DT; g += W) {
+      f32x4 vk, vv;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f, y = 0.f;
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f, y = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        x += part[w * PART + (4 * g + r) * 64 + lane];
-        y += part[w * PART + PART / 2 + (4 * g + r) * 64 + lane];
+        for (int w = 0; w < W; ++w) {
+          x += part[w * PART + (4 * g + r) * 64 + lane];
+          y += part[w * PART + PART / 2 + (4 * g + r) * 64 + lane];
+        }
+        vk[r] = x * scale;
+        vv[r] = y;
       }
-      vk[r] = x * scale;
-      vv[r] = y;
+      store4(to + 8 * g, vk);
+      store4(to + hkv + 8 * g, vv);
     }
-    store4(out + 8 * g, vk);
-    store4(out + hkv + 8 * g, vv);
   }
+  if (redo)
+    redo_packed_key_rows<bf16, DH>(share_of<W>(redo, wave), k0, plan, qkv, d_o, lse, from_delta, out, out + hkv, ld, h, hkv, group, group,
+                                   head0, scale, -1.f);
 }
 
 template <int DH>
 __global__ __launch_bounds__(64 * Few<DH>::W) void packed_few_bwd_kernel(const bf16* __restrict__ qkv, const int* words,
                                                                         const bf16* __restrict__ d_o, const float* __restrict__ lse,
-                                                                        const float* __restrict__ delta, bf16* __restrict__ dqkv,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv,
                                                                         int rows, int h, int hkv, int group, float scale,
                                                                         int dkv_blocks) {
   extern __shared__ __align__(16) char smem[];
@@ -337,16 +362,614 @@ __global__ __launch_bounds__(64 * Few<DH>::W) void packed_few_bwd_kernel(const b
   const bool dkv = (int)blockIdx.x < dkv_blocks;
   const int x = dkv ? blockIdx.x : blockIdx.x - dkv_blocks, n_x = dkv ? hkv / DH : h / DH, head = x % n_x, at = x / n_x;
   // of a block of 128 rows the first keys and the last queries meet the most
-  const int row0 = dkv ? plan.query_order()[at >> 2] * kPlanBlock + (at & 3) * kRows
-                       : plan.key_order()[at >> 2] * kPlanBlock + (3 - (at & 3)) * kRows;
+  const int row0 = dkv ? plan.query_order()[at >> 2].x * kPlanBlock + (at & 3) * kRows
+                       : plan.key_order()[at >> 2].x * kPlanBlock + (3 - (at & 3)) * kRows;
   if (row0 >= total) return;
   if (dkv)
-    packed_few_dkv_block<DH>(smem, row0, head, plan, total, qkv, d_o, lse, delta, dqkv, h, hkv, group, scale);
+    packed_few_dkv_block<DH>(smem, row0, head, plan, total, qkv, d_o, lse, from_lse, from_delta, dqkv, h, hkv, group, scale);
   else
-    packed_few_dq_block<DH>(smem, row0, head, plan, total, qkv, d_o, lse, delta, dqkv, h, hkv, group, scale);
+    packed_few_dq_block<DH>(smem, row0, head, plan, total, qkv, d_o, lse, from_lse, from_delta, dqkv, h, hkv, group, scale);
+}
+
+// ==================================================================================
+// Forward: four waves, each 32 rows against 32 keys at a time.
+// ==================================================================================
+
+// Consecutive blocks go to the eight XCDs in turn, each with an L2 of its own: heads that share keys and values go to the same one, next to
+// each other.
+__device__ __forceinline__ int head_of_block(int block, int n_heads, int group) {
+  const int x = block % n_heads;
+  return n_heads % 8 == 0 && group > 1 ? (x & 7) * (n_heads >> 3) + (x >> 3) : x;
+}
+
+// Rows row0 .. row0 + ROWS - 1 of the matrix at m into the tile at `tile`, by the four waves of a block; rows from `total` on become zeros.
+template <int DH, int ROWS>
+struct BlockLoads {
+  static constexpr int N = ROWS * DH * 2 / 4096;  // loads of a wave
+  unsigned off;
+  __device__ __forceinline__ BlockLoads(int ld, int wave, int lane) {
+    const int byte = wave * 1024 + lane * 16, row = byte / (DH * 2), c = (byte % (DH * 2) >> 4) ^ swz<DH>(row);
+    off = (unsigned)row * (unsigned)ld * 2u + c * 16;
+  }
+  __device__ __forceinline__ void request(char* tile, const bf16* m, int ld, int row0, int total, int wave) const {
+    const int left = min(total - row0, ROWS);
+    const i32x4 buf = buffer_of(m + (size_t)row0 * ld, left > 0 ? ((unsigned)(left - 1) * (unsigned)ld + DH) * 2u : 0u);
+    const unsigned lds = __builtin_amdgcn_readfirstlane((int)lds_byte(tile + wave * 1024));
+#pragma unroll
+    for (int u = 0; u < N; ++u) buffer_to_lds(lds + 4096u * u, off + (unsigned)(u * (4096 / (DH * 2))) * (unsigned)ld * 2u, buf);
+  }
+};
+
+// Where a lane reads fragments in a tile of 32 rows, as LDS bytes from the tile on: row fragments (contraction over the head dimension), step kk: row lane % 32;
+// transposing ones (contraction over the rows), block d of 32 columns: rows 4 (lane / 32) + .., the second half 8 rows further.  A step
+// or block on is an XOR of the chunk's bits: of the KEEP first steps (half blocks) kept in a register each, of the others formed at every read; everything else
+// is a constant of the instruction.
+template <int DH, int KEEP_ROW, int KEEP_COL>
+struct TileReads {
+  int row[KEEP_ROW], col[KEEP_COL];
+  __device__ __forceinline__ TileReads(int lane, int at) {
+    const int i = lane & 15, grp = lane >> 4, c = 16 * (grp & 1) + 4 * (i & 3);
+    const int k = at + tile_offset<DH>(lane & 31, lane >> 5), v = at + tile_offset<DH>(4 * (grp >> 1) + (i >> 2), c >> 3) + (c & 7) * 2;
+#pragma unroll
+    for (int x = 0; x < KEEP_ROW; ++x) row[x] = k ^ (x << 5);
+#pragma unroll
+    for (int x = 0; x < KEEP_COL; ++x) col[x] = v ^ (x << 5);  // 2 d + half: rows 8 further have their chunks 2 places on
+  }
+  template <int KEEP>
+  static __device__ __forceinline__ unsigned at(const int (&kept)[KEEP], int x) {
+    if (x < KEEP) return kept[x];
+    unsigned a;  // as text, or the compiler would keep it
+    asm volatile("v_xor_b32 %0, %1, %2" : "=v"(a) : "i"((x & -KEEP) << 5), "v"(kept[x & (KEEP - 1)]));
+    return a;
+  }
+  // `tile`: a constant number of bytes
+  __device__ __forceinline__ bf16x8 row_fragment(int tile, int kk) const {
+    typedef const __attribute__((address_space(3))) bf16x8* lds_ptr;
+    return *(lds_ptr)(size_t)(at(row, kk) + tile);
+  }
+  __device__ __forceinline__ bf16x8 col_fragment(int tile, int step, int d) const {
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    union {
+      s16x4 half[2];
+      bf16x8 v;
+    } u;
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(size_t)(at(col, 2 * d) + tile + step * 16 * DH * 2));
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(size_t)(at(col, 2 * d + 1) + tile + (step * 16 + 8) * DH * 2));
+    return u.v;
+  }
+};
+
+// SPLIT = 2: blocks of 64 rows, waves w and w + 2 own the same 32 and take one half of each stage's keys; merged through LDS at the end.
+template <int DH, int SPLIT, int SUB>
+__global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void packed_wide_fwd_kernel(const bf16* __restrict__ qkv, const int* words, bf16* __restrict__ o,
+                                                                  float* __restrict__ lse, int rows, int h, int hkv, int group,
+                                                                  float scale) {
+  constexpr int DT = DH / 32, KS = DH / 16, KT = 32 * SPLIT * SUB, BQ = 128 / SPLIT, TBYTES = KT * DH * 2, STAGE = 2 * TBYTES;
+  constexpr int RING = DH == 64 ? 8 : 4;  // fragments read ahead
+  using Loads = BlockLoads<DH, KT>;
+  extern __shared__ __align__(16) char smem[];
+  const PackedPlan plan{words, rows};
+  const int total = plan.total();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_heads = h / DH;
+  if (total == 0) return;
+  const int head = head_of_block(blockIdx.x, n_heads, group), at = blockIdx.x / n_heads;
+  const int2 block = plan.key_order()[at / SPLIT];
+  const int q0 = block.x * kPlanBlock + (SPLIT - 1 - at % SPLIT) * BQ;
+  if (q0 >= total) return;
+  const int last = total - 1, ld = h + 2 * hkv, half = lane >> 5, slice = wave / (4 / SPLIT);
+  const int qw0 = q0 + 32 * (wave % (4 / SPLIT)), q = qw0 + (lane & 31);
+  const int tile0 = (SPLIT == 1 ? block.y : plan.first()[q0]) / KT, n_tiles = min(q0 + BQ - 1, last) / KT + 1 - tile0;
+  const bf16* kbase = qkv + h + (head / group) * DH;
+  const Loads loads(ld, wave, lane);
+  auto load_stage = [&](int stage, int t) __attribute__((always_inline)) {
+    char* st = smem + stage * STAGE;
+    loads.request(st, kbase, ld, (tile0 + t) * KT, total, wave);
+    loads.request(st + TBYTES, kbase + hkv, ld, (tile0 + t) * KT, total, wave);
+  };
+  bf16x8 qf[KS];
+  load_row<DH>(qf, qkv + (size_t)min(q, last) * ld + head * DH, half);  // (rows past the end: computed, not stored)
+  const int first = plan.first()[q], first_hi = plan.first()[min(qw0 + 31, last)], first_lo = plan.first()[qw0];
+  load_stage(0, 0);
+  if (n_tiles > 1) load_stage(1, 1);
+  wait_loads_visibly();
+  const unsigned span = (unsigned)(q - first);
+  const float c = scale * kLog2e;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) acc[d] = zero16();
+  float ref = -INFINITY, l_run = 0.f;
+  const TileReads<DH, DH == 128 && SPLIT == 2 ? 4 : KS, DH == 128 ? 4 : KS> reads(lane, (int)lds_byte(smem) + slice * SUB * 32 * DH * 2);
+  auto tile = [&](auto stage, int t) __attribute__((always_inline)) {
+    if (t + 1 < n_tiles) wait_loads<2 * Loads::N>();
+    else wait_loads<0>();
+    __syncthreads();
+#pragma unroll
+    for (int sub = 0; sub < SUB; ++sub) {
+      const int ktile = decltype(stage)::value * STAGE + sub * 32 * DH * 2, vtile = ktile + TBYTES;
+      const int key0 = (tile0 + t) * KT + 32 * (slice * SUB + sub);
+      if (key0 > qw0 + 31 || key0 + 31 < first_lo || qw0 > last) continue;
+      // fragment f: rows of K for the scores, then columns of V
+      auto fragment = [&](int f) __attribute__((always_inline)) {
+        return f < KS ? reads.row_fragment(ktile, f) : reads.col_fragment(vtile, (f - KS) / DT, (f - KS) % DT);
+      };
+      bf16x8 ring[RING];
+#pragma unroll
+      for (int f = 0; f < RING; ++f) ring[f] = fragment(f);
+      f32x16 p = zero16();
+#pragma unroll
+      for (int m = 0; m < KS; ++m) {
+        p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[m % RING], qf[m], p, 0, 0, 0);
+        if (m + RING < KS + 2 * DT) ring[m % RING] = fragment(m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (key0 + 31 > qw0 || key0 < first_hi) {
+        const int rel = key0 + 4 * half - first;
+        asm volatile("");  // a branch: as selects every tile would pay for the mask
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((unsigned)(rel + 8 * (e >> 2) + (e & 3)) > span) p[e] = -INFINITY;
+      }
+      float mx = p[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, p[e]);
+      mx = exponent_of(fmaxf(mx, __shfl_xor(mx, 32, 64)), c);
+      const bool outgrown = __builtin_amdgcn_ballot_w64(mx - ref > 8.0f) != 0;
+      if (outgrown) {
+        const float now = fmaxf(ref, mx), alpha = fast_exp2(ref - (now == -INFINITY ? 0.f : now));
+        ref = now;
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+      }
+      const float to = ref == -INFINITY ? 0.f : ref;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = fast_exp2(fmaf(p[e], c, -to));
+        sum += p[e];
+      }
+      l_run += sum;
+      const bf16x8 pf[2] = {pack_bf16x8(p, 0), pack_bf16x8(p, 8)};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 2 * DT; ++m) {
+        acc[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(KS + m) % RING], pf[m / DT], acc[m % DT], 0, 0, 0);
+        if (m + RING < 2 * DT) ring[(KS + m) % RING] = fragment(KS + m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (t + 2 < n_tiles) {
+      __syncthreads();
+      load_stage(decltype(stage)::value, t + 2);
+    }
+  };
+  for (int t = 0; t < n_tiles; t += 2)
+    static_for<0, 2>([&](auto stage) __attribute__((always_inline)) {
+      if (t + decltype(stage)::value < n_tiles) tile(stage, t + decltype(stage)::value);
+    });
+  float l = l_run + __shfl_xor(l_run, 32, 64);
+  if constexpr (SPLIT == 2) {
+    float* xch = reinterpret_cast<float*>(smem) + (wave & 1) * (64 * (DT * 16 + 2));
+    __syncthreads();
+    if (slice == 1) {
+      put_partial<DT>(xch, acc, lane);
+      xch[(DT * 16) * 64 + lane] = ref;
+      xch[(DT * 16 + 1) * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (slice == 1) return;
+    const float ref1 = xch[(DT * 16) * 64 + lane], l1 = xch[(DT * 16 + 1) * 64 + lane], to = fmaxf(ref, ref1);
+    const float a0 = fast_exp2(ref - to), a1 = fast_exp2(ref1 - to);
+    l = l * a0 + l1 * a1;
+    ref = to;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = acc[d][e] * a0 + xch[(d * 16 + e) * 64 + lane] * a1;
+  }
+  const uint32_t redo = rows_to_redo(not_finite<DT>(acc) && !is_nan(l), total - qw0);
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc[d][4 * b + r] * inv;
+        store4(o + (size_t)q * h + head * DH + 32 * d + 8 * b + 4 * half, v);
+      }
+  }
+  if (q <= last && half == 0) lse[(size_t)head * rows + q] = fmaf(ref, 0.6931471805599453f, __logf(l));
+  if (redo) redo_packed_forward_rows<bf16, DH>(redo, qw0, plan, qkv, o, h, hkv, group, head, scale);
+}
+
+// ==================================================================================
+// Backward.  dQ blocks own rows, dK/dV blocks keys, 32 a wave; both form S and dP again:
+//   P = exp(S scale - lse), dS = P (dP - delta), dQ = dS K scale, dK = dS^T Q scale, dV = P^T dO.
+// ==================================================================================
+
+// 128 / SPLIT query rows of a head from q0 on, key0 the first key that they see.  SPLIT as in the forward.
+template <int DH, int SPLIT, int NST>
+__device__ __forceinline__ void packed_dq_block(char* smem, int q0, int key_first, int head, PackedPlan plan, int total,
+                                                const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
+                                                const float* __restrict__ lse,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
+                                                bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+  constexpr int DT = DH / 32, KS = DH / 16, KT = 32 * SPLIT, BQ = 128 / SPLIT, TBYTES = KT * DH * 2, STAGE = 2 * TBYTES, RING = DH == 128 ? 8 : 4;
+  using Loads = BlockLoads<DH, KT>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int last = total - 1, ld = h + 2 * hkv, slice = wave / (4 / SPLIT);
+  const int qw0 = q0 + 32 * (wave % (4 / SPLIT)), q = qw0 + (lane & 31), qc = min(q, last);
+  const int tile0 = key_first / KT, n_tiles = min(q0 + BQ - 1, last) / KT + 1 - tile0;
+  const bf16* kbase = qkv + h + (head / group) * DH;
+  const Loads loads(ld, wave, lane);
+  auto load_stage = [&](int stage, int t) __attribute__((always_inline)) {
+    char* st = smem + stage * STAGE;
+    loads.request(st, kbase, ld, (tile0 + t) * KT, total, wave);
+    loads.request(st + TBYTES, kbase + hkv, ld, (tile0 + t) * KT, total, wave);
+  };
+  bf16x8 qf[KS], dof[KS];
+  load_row<DH>(qf, qkv + (size_t)qc * ld + head * DH, half);  // (rows past the end: computed, not stored)
+  load_row<DH>(dof, d_o + (size_t)qc * h + head * DH, half);
+  const float c = scale * kLog2e;
+  const float lse_q = from_lse[(size_t)head * plan.rows + qc] * -c, delta_q = -from_delta[(size_t)head * plan.rows + qc];
+  const int first = plan.first()[q], first_hi = plan.first()[min(qw0 + 31, last)], first_lo = plan.first()[min(qw0, last)];
+  load_stage(0, 0);
+  if (n_tiles > 1) load_stage(1, 1);
+  wait_loads_visibly();
+  const unsigned span = (unsigned)(q - first);
+  f32x16 dq[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) dq[d] = zero16();
+  const TileReads<DH, KS, KS> reads(lane, (int)lds_byte(smem) + slice * 32 * DH * 2);
+  auto tile = [&](auto stage, int t) __attribute__((always_inline)) {
+    if (t + 1 < n_tiles) wait_loads<2 * Loads::N>();
+    else wait_loads<0>();
+    __syncthreads();
+    if (NST == 3 && t + 2 < n_tiles) load_stage((decltype(stage)::value + 2) % 3, t + 2);
+    const int ktile = decltype(stage)::value * STAGE, vtile = ktile + TBYTES, key0 = (tile0 + t) * KT + 32 * slice;
+    if (key0 <= qw0 + 31 && key0 + 31 >= first_lo && qw0 <= last) {
+      // fragment f: of K and of V in turn for the scores and dP, then columns of K
+      auto fragment = [&](int f) __attribute__((always_inline)) {
+        if (f < 2 * KS) return reads.row_fragment(f & 1 ? vtile : ktile, f >> 1);
+        return reads.col_fragment(ktile, (f - 2 * KS) / DT, (f - 2 * KS) % DT);
+      };
+      bf16x8 ring[RING];
+#pragma unroll
+      for (int f = 0; f < RING; ++f) ring[f] = fragment(f);
+      f32x16 p = zero16(), ds = zero16();
+#pragma unroll
+      for (int m = 0; m < 2 * KS; ++m) {
+        if (m & 1) ds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[m % RING], dof[m >> 1], ds, 0, 0, 0);
+        else p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[m % RING], qf[m >> 1], p, 0, 0, 0);
+        if (m + RING < 2 * KS + 2 * DT) ring[m % RING] = fragment(m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = fast_exp2(fmaf(p[e], c, -lse_q));
+        ds[e] = p[e] * (ds[e] - delta_q);
+      }
+      if (key0 + 31 > qw0 || key0 < first_hi) {
+        const int rel = key0 + 4 * half - first;
+        asm volatile("");  // a branch: as selects every tile would pay for the mask
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((unsigned)(rel + 8 * (e >> 2) + (e & 3)) > span) ds[e] = 0.f;
+      }
+      const bf16x8 dsf[2] = {pack_bf16x8(ds, 0), pack_bf16x8(ds, 8)};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 2 * DT; ++m) {
+        dq[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], dsf[m / DT], dq[m % DT], 0, 0, 0);
+        if (m + RING < 2 * DT) ring[(2 * KS + m) % RING] = fragment(2 * KS + m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (NST == 2 && t + 2 < n_tiles) {
+      __syncthreads();
+      load_stage(decltype(stage)::value, t + 2);
+    }
+  };
+  for (int t = 0; t < n_tiles; t += NST)
+    static_for<0, NST>([&](auto stage) __attribute__((always_inline)) {
+      if (t + decltype(stage)::value < n_tiles) tile(stage, t + decltype(stage)::value);
+    });
+  if constexpr (SPLIT == 2) {
+    float* xch = reinterpret_cast<float*>(smem) + (wave & 1) * (64 * DT * 16);
+    __syncthreads();
+    if (slice == 1) put_partial<DT>(xch, dq, lane);
+    __syncthreads();
+    if (slice == 1) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dq[d][e] += xch[(d * 16 + e) * 64 + lane];
+  }
+  const uint32_t redo = rows_to_redo(not_finite<DT>(dq) && !is_nan(lse_q + delta_q), total - qw0);
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = dq[d][4 * b + r] * scale;
+        store4(dqkv + (size_t)q * ld + head * DH + 32 * d + 8 * b + 4 * half, v);
+      }
+  }
+  if (redo) redo_packed_dq_rows<bf16, DH>(redo, qw0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
+}
+
+// 128 / SPLIT keys of a key/value head from k0 on, `end` the row behind the last that sees one of them; walks the query tiles of every head of the
+// group.  Heads of 128: the last V fragments stand in LDS, a place per lane, for want of registers.
+template <int DH, int SPLIT, int NST>
+struct KeyBlock {
+  static constexpr int KT = 32 * SPLIT, TBYTES = KT * DH * 2, STATS = 4 * 256, STAGE = 2 * TBYTES + STATS;
+  static constexpr int V_IN_LDS = DH == 128 ? (SPLIT == 1 ? 4 : 3) : 0, V_AT = NST * STAGE, BYTES = V_AT + 4 * V_IN_LDS * 1024;
+};
+template <int DH, int SPLIT, int NST>
+__device__ __forceinline__ void packed_dkv_block(char* smem, int k0, int query_end, int kv_head, PackedPlan plan, int total,
+                                                 const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
+                                                 const float* __restrict__ lse,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
+                                                 bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+  using B = KeyBlock<DH, SPLIT, NST>;
+  constexpr int DT = DH / 32, KS = DH / 16, KT = B::KT, TBYTES = B::TBYTES, RING = 3, V_IN_REG = KS - B::V_IN_LDS;
+  using Loads = BlockLoads<DH, KT>;
+  int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int last = total - 1, ld = h + 2 * hkv, slice = wave / (4 / SPLIT), head0 = kv_head * group;
+  const int kw0 = k0 + 32 * (wave % (4 / SPLIT));
+  int key = kw0 + (lane & 31);
+  const int tile0 = k0 / KT, n_q = (query_end - 1) / KT + 1 - tile0, n_it = group * n_q;
+  const Loads q_loads(ld, wave, lane), do_loads(h, wave, lane);
+  const float* stat_of = half ? from_delta : from_lse;
+  int g_next = 0, t_next = 0;  // the next tile to ask for
+  auto load_stage = [&](int stage) __attribute__((always_inline)) {
+    char* st = smem + stage * B::STAGE;
+    const int head = head0 + g_next, row0 = (tile0 + t_next) * KT;
+    q_loads.request(st, qkv + head * DH, ld, row0, total, wave);
+    do_loads.request(st + TBYTES, d_o + head * DH, h, row0, total, wave);
+    // the statistics of the 32 rows that this wave takes, in a place of its own
+    float_to_lds(__builtin_amdgcn_readfirstlane((int)lds_byte(st + 2 * TBYTES + wave * 256)),
+                 stat_of + (size_t)head * plan.rows + min(row0 + 32 * slice + (lane & 31), last));
+    if (++t_next == n_q) t_next = 0, ++g_next;
+  };
+  bf16x8 kf[KS], vf[V_IN_REG];
+  char* vslot = smem + B::V_AT + (wave * B::V_IN_LDS * 64 + lane) * 16;
+  {
+    const bf16* krow = qkv + (size_t)min(key, last) * ld + h + kv_head * DH;  // (keys past the end: computed, not stored)
+    load_row<DH>(kf, krow, half);
+    bf16x8 v[KS];
+    load_row<DH>(v, krow + hkv, half);
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      if (kk < V_IN_REG) vf[kk] = v[kk];
+      else *reinterpret_cast<bf16x8*>(vslot + (kk - V_IN_REG) * 1024) = v[kk];
+    }
+  }
+  const int end = plan.end()[key], end_lo = plan.end()[min(kw0, last)], end_hi = plan.end()[min(kw0 + 31, last)];
+  load_stage(0);
+  if (n_it > 1) load_stage(1);
+  wait_loads_visibly();
+  const float c = scale * kLog2e;
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) dk[d] = dv[d] = zero16();
+  int t_now = 0;
+  auto tile = [&](auto stage, int it) __attribute__((always_inline)) {
+    constexpr int kLoads = 2 * Loads::N + 1;
+    if (it + 1 < n_it) wait_loads<kLoads>();
+    else wait_loads<0>();
+    __syncthreads();
+    if (NST == 3 && it + 2 < n_it) load_stage((decltype(stage)::value + 2) % 3);
+    const int q0 = (tile0 + t_now) * KT + 32 * slice;
+    if (++t_now == n_q) t_now = 0;
+    if (q0 + 31 >= kw0 && q0 < end_hi && kw0 <= last) {
+      int lane_l = lane;
+      asm volatile("" : "+v"(lane_l));  // addresses are formed again rather than kept across tiles, where every register is taken
+      const TileReads<DH, 2, 2> reads(lane_l, (int)lds_byte(smem) + decltype(stage)::value * B::STAGE + slice * 32 * DH * 2);
+      const char* vslot_l = smem + B::V_AT + (wave * B::V_IN_LDS * 64 + lane_l) * 16;
+      const float* stat = reinterpret_cast<const float*>(smem + decltype(stage)::value * B::STAGE + 2 * TBYTES + wave * 256);
+      const int half_l = lane_l >> 5;
+      // fragment f: of Q and of dO in turn for the scores and dP, then columns of dO and of Q in turn
+      auto fragment = [&](int f) __attribute__((always_inline)) {
+        if (f < 2 * KS) return reads.row_fragment(f & 1 ? TBYTES : 0, f >> 1);
+        f -= 2 * KS;
+        return reads.col_fragment(f & 1 ? 0 : TBYTES, (f >> 1) / DT, (f >> 1) % DT);
+      };
+      bf16x8 ring[RING];
+#pragma unroll
+      for (int f = 0; f < RING; ++f) ring[f] = fragment(f);
+      f32x16 p, ds;  // the row statistics are the initial value: S - lse / scale and dP - delta
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {  // register 4 b + r is query row 8 b + 4 half + r
+        const f32x4 vl = *reinterpret_cast<const f32x4*>(stat + 8 * b + 4 * half_l);
+        const f32x4 vd = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * b + 4 * half_l);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[4 * b + r] = vl[r];
+          ds[4 * b + r] = vd[r];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 2 * KS; ++m) {
+        if (m & 1) {
+          bf16x8 v;
+          if ((m >> 1) < V_IN_REG) v = vf[m >> 1];
+          else v = *reinterpret_cast<const bf16x8*>(vslot_l + ((m >> 1) - V_IN_REG) * 1024);
+          ds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[m % RING], v, ds, 0, 0, 0);
+        } else {
+          p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[m % RING], kf[m >> 1], p, 0, 0, 0);
+        }
+        ring[m % RING] = fragment(m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = fast_exp2(p[e] * c);
+        ds[e] *= p[e];
+      }
+      if (q0 < kw0 + 31 || q0 + 32 > end_lo) {  // the diagonal, or rows past the end of a sequence
+        const int rel = q0 + 4 * half - key;
+        const unsigned span = (unsigned)(end - key);
+        asm volatile("");  // a branch: as selects every tile would pay for the mask
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((unsigned)(rel + 8 * (e >> 2) + (e & 3)) >= span) p[e] = ds[e] = 0.f;  // dS too: 0 times a dP that is not finite is no 0
+      }
+      const bf16x8 w[2][2] = {{pack_bf16x8(p, 0), pack_bf16x8(ds, 0)}, {pack_bf16x8(p, 8), pack_bf16x8(ds, 8)}};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 4 * DT; ++m) {
+        const int step = (m >> 1) / DT, d = (m >> 1) % DT;
+        if (m & 1) dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], w[step][1], dk[d], 0, 0, 0);
+        else dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], w[step][0], dv[d], 0, 0, 0);
+        if (m + RING < 4 * DT) ring[(2 * KS + m) % RING] = fragment(2 * KS + m + RING);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (NST == 2 && it + 2 < n_it) {
+      __syncthreads();
+      load_stage(decltype(stage)::value);
+    }
+  };
+  for (int it = 0; it < n_it; it += NST)
+    static_for<0, NST>([&](auto stage) __attribute__((always_inline)) {
+      if (it + decltype(stage)::value < n_it) tile(stage, it + decltype(stage)::value);
+    });
+  // rebuilt rather than kept across the loop
+  lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  half = lane >> 5;
+  key = kw0 + (lane & 31);
+  if constexpr (SPLIT == 2) {
+    float* xch = reinterpret_cast<float*>(smem) + (wave & 1) * (2 * 64 * DT * 16);
+    __syncthreads();
+    if (slice == 1) {
+      put_partial<DT>(xch, dk, lane);
+      put_partial<DT>(xch + 64 * DT * 16, dv, lane);
+    }
+    __syncthreads();
+    if (slice == 1) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        dk[d][e] += xch[(d * 16 + e) * 64 + lane];
+        dv[d][e] += xch[((DT + d) * 16 + e) * 64 + lane];
+      }
+  }
+  bf16* out = dqkv + h + kv_head * DH;
+  const size_t stat_at = (size_t)head0 * plan.rows;
+  const uint32_t redo = keys_to_redo(rows_to_redo(not_finite<DT>(dk), total - kw0), rows_to_redo(not_finite<DT>(dv), total - kw0), lse + stat_at,
+                                     from_delta + stat_at, min(key, last), group, plan.rows);
+  if (key <= last && !(redo >> (lane & 31) & 1)) {
+    bf16* to = out + (size_t)key * ld + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        f32x4 vk, vv;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          vk[r] = dk[d][4 * b + r] * scale;
+          vv[r] = dv[d][4 * b + r];
+        }
+        store4(to + 32 * d + 8 * b, vk);
+        store4(to + hkv + 32 * d + 8 * b, vv);
+      }
+  }
+  if (redo)
+    redo_packed_key_rows<bf16, DH>(redo, kw0, plan, qkv, d_o, lse, from_delta, out, out + hkv, ld, h, hkv, group, group, head0,
+                                   scale, -1.f);
+}
+
+template <int DH, int SPLIT, int NST>
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_wide_bwd_kernel(const bf16* __restrict__ qkv, const int* words,
+                                                                  const bf16* __restrict__ d_o, const float* __restrict__ lse,
+                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int rows,
+                                                                  int h, int hkv, int group, float scale, int dkv_blocks) {
+  extern __shared__ __align__(16) char smem[];
+  const PackedPlan plan{words, rows};
+  const int total = plan.total();
+  if (total == 0) return;
+  // dK/dV blocks first: the dQ blocks start on the CUs that light ones leave early
+  if ((int)blockIdx.x < dkv_blocks) {
+    const int n_kv = hkv / DH, at = blockIdx.x / n_kv;
+    const int2 block = plan.query_order()[at / SPLIT];
+    const int k0 = block.x * kPlanBlock + at % SPLIT * (128 / SPLIT);
+    if (k0 >= total) return;
+    const int end = SPLIT == 1 ? block.y : plan.end()[min(k0 + 128 / SPLIT, total) - 1];
+    packed_dkv_block<DH, SPLIT, NST>(smem, k0, end, blockIdx.x % n_kv, plan, total, qkv, d_o, lse, from_lse, from_delta, dqkv, h, hkv, group, scale);
+  } else {
+    const int x = blockIdx.x - dkv_blocks, n_heads = h / DH, at = x / n_heads;
+    const int2 block = plan.key_order()[at / SPLIT];
+    const int q0 = block.x * kPlanBlock + (SPLIT - 1 - at % SPLIT) * (128 / SPLIT);
+    if (q0 >= total) return;
+    packed_dq_block<DH, SPLIT, NST>(smem, q0, SPLIT == 1 ? block.y : plan.first()[q0], head_of_block(x, n_heads, group), plan, total, qkv,
+                                    d_o, lse, from_lse, from_delta, dqkv, h, hkv, group, scale);
+  }
+}
+
+// What the backward adds to scores and to dP, as the initial value of their accumulators: from_lse = -lse / scale and from_delta = -delta,
+// delta = dO . O of a row and head; DH / 8 lanes a row and head, 16 bytes of both per lane.
+template <int DH>
+__global__ __launch_bounds__(256) void packed_stats_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o,
+                                                           const float* __restrict__ lse, float* __restrict__ from_lse,
+                                                           float* __restrict__ from_delta, int rows, int h, float to_lse) {
+  constexpr int LANES = DH / 8;
+  const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x, pair = t / LANES;
+  const unsigned n_heads = h / DH, row = (unsigned)(pair / n_heads), head = (unsigned)(pair - (size_t)row * n_heads);
+  float d = 0.f;
+  if (row < (unsigned)rows) {
+    const bf16x8 a = *reinterpret_cast<const bf16x8*>(o + t * 8), b = *reinterpret_cast<const bf16x8*>(d_o + t * 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d = fmaf((float)a[e], (float)b[e], d);
+  }
+#pragma unroll
+  for (int m = 1; m < LANES; m <<= 1) d += __shfl_xor(d, m);
+  if (row < (unsigned)rows && threadIdx.x % LANES == 0) {
+    const size_t at = (size_t)head * rows + row;
+    from_lse[at] = lse[at] * to_lse;
+    from_delta[at] = -d;
+  }
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------
+template <int DH>
+static bool statistics(const bf16* o, const bf16* d_o, const float* lse, float* stats, int rows, int h, int n_heads, hipStream_t stream) {
+  packed_stats_kernel<DH><<<(unsigned)(((size_t)rows * h / 8 + 255) / 256), 256, 0, stream>>>(
+      o, d_o, lse, stats, stats + (size_t)n_heads * rows, rows, h, -sqrtf((float)DH));
+  return launch_ok("packed_stats_kernel");
+}
+
+template <int DH, int SPLIT, int NST>
+static bool wide_backward(const bf16* qkv, const int* plan, const float* lse, const float* stats, const bf16* d_o, bf16* dqkv, int rows,
+                           int h, int n_heads, int n_kv_heads, hipStream_t stream) {
+  constexpr int dq = NST * 2 * 32 * SPLIT * DH * 2, dkv = KeyBlock<DH, SPLIT, NST>::BYTES, merge = SPLIT == 2 ? 4 * 64 * (DH / 32) * 16 * 4 : 0;
+  constexpr int smem = dkv > merge ? (dkv > dq ? dkv : dq) : (merge > dq ? merge : dq);
+  static LdsLimit lds;
+  if (!lds.allow(packed_wide_bwd_kernel<DH, SPLIT, NST>, smem)) return false;
+  const int blocks = ceil_div(rows, kPlanBlock) * SPLIT;
+  packed_wide_bwd_kernel<DH, SPLIT, NST><<<(n_kv_heads + n_heads) * blocks, 256, smem, stream>>>(
+      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * blocks);
+  return launch_ok("packed_wide_bwd_kernel");
+}
+template <int DH, int SPLIT, int SUB>
+static bool wide_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, int rows, int h, int n_heads, int n_kv_heads,
+                          hipStream_t stream) {
+  constexpr int smem = 2 * 2 * 32 * SPLIT * SUB * DH * 2;
+  static LdsLimit lds;
+  if (!lds.allow(packed_wide_fwd_kernel<DH, SPLIT, SUB>, smem)) return false;
+  packed_wide_fwd_kernel<DH, SPLIT, SUB><<<n_heads * ceil_div(rows, kPlanBlock) * SPLIT, 256, smem, stream>>>(
+      qkv, plan, o, lse, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH));
+  return launch_ok("packed_wide_fwd_kernel");
+}
 template <int DH>
 static bool few_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, int rows, int h, int n_heads, int n_kv_heads,
                         hipStream_t stream) {
@@ -360,15 +983,15 @@ static bool few_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, i
 }
 
 template <int DH>
-static bool few_backward(const bf16* qkv, const int* plan, const float* lse, const float* delta, const bf16* d_o, bf16* dqkv, int rows,
+static bool few_backward(const bf16* qkv, const int* plan, const float* lse, const float* stats, const bf16* d_o, bf16* dqkv, int rows,
                          int h, int n_heads, int n_kv_heads, hipStream_t stream) {
   using F = Few<DH>;
-  constexpr int smem = F::AFTER + F::W * F::NS * 256 + F::W * 4;
+  constexpr int smem = F::AFTER + F::W * F::NS * 256 + 2 * F::W * 4;
   static LdsLimit lds;
   if (!lds.allow(packed_few_bwd_kernel<DH>, smem)) return false;
   const int tiles = ceil_div(rows, kPlanBlock) * 4;
   packed_few_bwd_kernel<DH><<<(n_kv_heads + n_heads) * tiles, 64 * F::W, smem, stream>>>(
-      qkv, plan, d_o, lse, delta, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * tiles);
+      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * tiles);
   return launch_ok("packed_few_bwd_kernel");
 }
 
@@ -401,13 +1024,15 @@ bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void*
     return false;
   if (dtype == kF32)
     return attention_packed_forward_f32((const float*)qkv, plan, (float*)o, lse, rows, h, n_heads, n_kv_heads, stream);
-  auto launch = h / n_heads == 128 ? few_forward<128> : few_forward<64>;
+  const int64_t blocks = (int64_t)n_heads * ceil_div(rows, kPlanBlock);
+  auto launch = h / n_heads == 128 ? (blocks <= 64 ? few_forward<128> : blocks <= 384 ? wide_forward<128, 2, 1> : wide_forward<128, 1, 1>)
+                                   : (blocks <= 64 ? few_forward<64> : blocks <= 512 ? wide_forward<64, 2, 1> : wide_forward<64, 1, 2>);
   return launch((const bf16*)qkv, plan, (bf16*)o, lse, rows, h, n_heads, n_kv_heads, stream);
 }
 
 size_t attention_packed_backward_workspace(int dtype, int rows, int h, int n_heads, int n_kv_heads) {
-  (void)dtype, (void)h, (void)n_kv_heads;
-  return (size_t)n_heads * rows * sizeof(float);  // delta
+  (void)h, (void)n_kv_heads;
+  return (size_t)n_heads * rows * sizeof(float) * (dtype == kBF16 ? 2 : 1);  // delta, and in bf16 the scaled lse
 }
 
 bool attention_packed_backward(int dtype, const void* qkv, const int* plan, const void* o, const float* lse, const void* d_o,
@@ -416,14 +1041,20 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
              (uintptr_t)qkv | (uintptr_t)o | (uintptr_t)d_o | (uintptr_t)dqkv | (uintptr_t)workspace,
              !qkv || !plan || !o || !lse || !d_o || !dqkv || !workspace, (uintptr_t)lse))
     return false;
-  float* delta = (float*)workspace;
+  float* stats = (float*)workspace;
   if (dtype == kF32)
-    return attention_delta_f32((const float*)o, (const float*)d_o, delta, rows, h, n_heads, stream) &&
-           attention_packed_backward_f32((const float*)qkv, plan, lse, delta, (const float*)d_o, (float*)dqkv, rows, h, n_heads,
+    return attention_delta_f32((const float*)o, (const float*)d_o, stats, rows, h, n_heads, stream) &&
+           attention_packed_backward_f32((const float*)qkv, plan, lse, stats, (const float*)d_o, (float*)dqkv, rows, h, n_heads,
                                          n_kv_heads, stream);
-  if (!attention_delta_bf16((const bf16*)o, (const bf16*)d_o, delta, rows, h, n_heads, stream)) return false;
-  auto launch = h / n_heads == 128 ? few_backward<128> : few_backward<64>;
-  return launch((const bf16*)qkv, plan, lse, delta, (const bf16*)d_o, (bf16*)dqkv, rows, h, n_heads, n_kv_heads, stream);
+  if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, h, n_heads, stream))
+    return false;
+  const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);
+  const bool few = (int64_t)n_heads * row_blocks <= std::min(32 * group, 128);
+  auto launch = h / n_heads == 64                       ? (few ? few_backward<64> : wide_backward<64, 2, 2>)
+                : few                                   ? few_backward<128>
+                : (int64_t)n_kv_heads * row_blocks <= 256 ? wide_backward<128, 2, 2>
+                                                        : wide_backward<128, 1, 3>;
+  return launch((const bf16*)qkv, plan, lse, stats, (const bf16*)d_o, (bf16*)dqkv, rows, h, n_heads, n_kv_heads, stream);
 }
 
 }  // namespace po

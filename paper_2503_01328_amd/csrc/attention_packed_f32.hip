@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256, 2) void packed_f32_fwd_kernel(const float* __r
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int n_heads = h / DH, head = blockIdx.x % n_heads, at = blockIdx.x / n_heads;
   if (total == 0) return;
-  const int q0 = plan.key_order()[at >> 2] * kPlanBlock + (3 - (at & 3)) * 32;
+  const int q0 = plan.key_order()[at >> 2].x * kPlanBlock + (3 - (at & 3)) * 32;
   if (q0 >= total) return;
   const int q = q0 + (lane & 31), ld = h + 2 * hkv, last = total - 1;
   const int first = plan.first()[q], first_lo = plan.first()[q0], first_hi = plan.first()[min(q0 + 31, last)];
@@ -89,21 +89,22 @@ __global__ __launch_bounds__(256, 2) void packed_f32_fwd_kernel(const float* __r
     l += stat[(4 + w) * 64 + lane] * f[w];
   }
   const uint32_t redo = all_redo(redo_of) & rows_to_redo(!is_nan(l), 32);
-  if (redo) redo_packed_forward_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, o, lse, h, hkv, group, head, scale);
-  if (q > last || (redo >> (lane & 31) & 1)) return;
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
 #pragma unroll
-  for (int d = 0; d < DT; ++d) {
-    f32x4 v;
+    for (int d = 0; d < DT; ++d) {
+      f32x4 v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f;
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) x += lds[w * PART + (d * 16 + 4 * wave + r) * 64 + lane] * f[w];
-      v[r] = x / l;
+        for (int w = 0; w < 4; ++w) x += lds[w * PART + (d * 16 + 4 * wave + r) * 64 + lane] * f[w];
+        v[r] = x / l;
+      }
+      *reinterpret_cast<f32x4*>(o + (size_t)q * h + head * DH + 32 * d + 8 * wave + 4 * half) = v;
     }
-    *reinterpret_cast<f32x4*>(o + (size_t)q * h + head * DH + 32 * d + 8 * wave + 4 * half) = v;
   }
-  if (wave == 0 && half == 0) lse[(size_t)head * rows + q] = fmaf(m, scale, __logf(l));
+  if (wave == 0 && half == 0 && q <= last) lse[(size_t)head * rows + q] = fmaf(m, scale, __logf(l));
+  if (redo) redo_packed_forward_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, o, h, hkv, group, head, scale);
 }
 
 // 32 query rows of a head from q0 on.
@@ -155,20 +156,21 @@ __device__ __forceinline__ void packed_f32_dq_block(float* lds, int q0, int head
   if (lane == 0) redo_of[wave] = redo_mine;
   __syncthreads();
   const uint32_t redo = all_redo(redo_of);
-  if (redo) redo_packed_dq_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, d_o, lse, delta, dqkv, h, hkv, group, head, scale);
-  if (q > last || (redo >> (lane & 31) & 1)) return;
+  if (q <= last && !(redo >> (lane & 31) & 1)) {
 #pragma unroll
-  for (int d = 0; d < DT; ++d) {
-    f32x4 v;
+    for (int d = 0; d < DT; ++d) {
+      f32x4 v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f;
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) x += lds[w * PART + (d * 16 + 4 * wave + r) * 64 + lane];
-      v[r] = x * scale;
+        for (int w = 0; w < 4; ++w) x += lds[w * PART + (d * 16 + 4 * wave + r) * 64 + lane];
+        v[r] = x * scale;
+      }
+      *reinterpret_cast<f32x4*>(dqkv + (size_t)q * ld + head * DH + 32 * d + 8 * wave + 4 * half) = v;
     }
-    *reinterpret_cast<f32x4*>(dqkv + (size_t)q * ld + head * DH + 32 * d + 8 * wave + 4 * half) = v;
   }
+  if (redo) redo_packed_dq_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, d_o, lse, delta, dqkv, h, hkv, group, head, scale, 1.f);
 }
 
 // 32 keys of a key/value head from k0 on; its waves walk the query tiles of every query head that reads it.
@@ -230,33 +232,35 @@ __device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int kv_
   put_partial<DT>(lds + wave * 2 * PART, dk, lane);
   put_partial<DT>(lds + wave * 2 * PART + PART, dv, lane);
   uint32_t* redo_of = reinterpret_cast<uint32_t*>(lds + 8 * PART);
-  const uint32_t mine = rows_to_redo(not_finite<DT>(dk) || not_finite<DT>(dv), total - k0);
-  if (lane == 0) redo_of[wave] = mine;
+  const uint32_t bad_k = rows_to_redo(not_finite<DT>(dk), total - k0), bad_v = rows_to_redo(not_finite<DT>(dv), total - k0);
+  if (lane == 0) redo_of[wave] = bad_k, redo_of[4 + wave] = bad_v;
   __syncthreads();
   float* out = dqkv + h + kv_head * DH;
-  const uint32_t redo = all_redo(redo_of);
+  const size_t stat_at = (size_t)head0 * plan.rows;
+  const uint32_t redo = keys_to_redo(all_redo(redo_of), all_redo(redo_of + 4), lse + stat_at, delta + stat_at, min(key, last), group, plan.rows);
+  if (key <= last && !(redo >> (lane & 31) & 1)) {
+    float* to = out + (size_t)key * ld + 8 * wave + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      f32x4 vk, vv;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          x += lds[w * 2 * PART + (d * 16 + 4 * wave + r) * 64 + lane];
+          y += lds[w * 2 * PART + PART + (d * 16 + 4 * wave + r) * 64 + lane];
+        }
+        vk[r] = x * scale;
+        vv[r] = y;
+      }
+      *reinterpret_cast<f32x4*>(to + 32 * d) = vk;
+      *reinterpret_cast<f32x4*>(to + hkv + 32 * d) = vv;
+    }
+  }
   if (redo)
     redo_packed_key_rows<float, DH>(share_of(redo, wave), k0, plan, qkv, d_o, lse, delta, out, out + hkv, ld, h, hkv, group, group, head0,
-                                    scale);
-  if (key > last || (redo >> (lane & 31) & 1)) return;
-  out += (size_t)key * ld + 8 * wave + 4 * half;
-#pragma unroll
-  for (int d = 0; d < DT; ++d) {
-    f32x4 vk, vv;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = 0.f, y = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        x += lds[w * 2 * PART + (d * 16 + 4 * wave + r) * 64 + lane];
-        y += lds[w * 2 * PART + PART + (d * 16 + 4 * wave + r) * 64 + lane];
-      }
-      vk[r] = x * scale;
-      vv[r] = y;
-    }
-    *reinterpret_cast<f32x4*>(out + 32 * d) = vk;
-    *reinterpret_cast<f32x4*>(out + hkv + 32 * d) = vv;
-  }
+                                    scale, 1.f);
 }
 
 template <int DH>
@@ -273,8 +277,8 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void packed_f32_bwd_kernel(co
   const bool dkv = (int)blockIdx.x < dkv_blocks;
   const int x = dkv ? blockIdx.x : blockIdx.x - dkv_blocks, n_x = dkv ? hkv / DH : h / DH, head = x % n_x, at = x / n_x;
   // of a block of 128 rows the first keys and the last queries meet the most
-  const int row0 = dkv ? plan.query_order()[at >> 2] * kPlanBlock + (at & 3) * 32
-                       : plan.key_order()[at >> 2] * kPlanBlock + (3 - (at & 3)) * 32;
+  const int row0 = dkv ? plan.query_order()[at >> 2].x * kPlanBlock + (at & 3) * 32
+                       : plan.key_order()[at >> 2].x * kPlanBlock + (3 - (at & 3)) * 32;
   if (row0 >= total) return;
   if (dkv)
     packed_f32_dkv_block<DH>(lds, row0, head, plan, total, qkv, d_o, lse, delta, dqkv, h, hkv, group, scale);
@@ -297,7 +301,7 @@ static bool forward_f32(const float* qkv, const int* plan, float* o, float* lse,
 template <int DH>
 static bool backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o, float* dqkv, int rows,
                          int h, int n_heads, int n_kv_heads, hipStream_t stream) {
-  constexpr int smem = 8 * kTileBytes<DH> + 16;
+  constexpr int smem = 8 * kTileBytes<DH> + 32;
   static LdsLimit lds;
   if (!lds.allow(packed_f32_bwd_kernel<DH>, smem)) return false;
   const int tiles = ceil_div(rows, kPlanBlock) * 4;

@@ -186,11 +186,11 @@ __device__ __forceinline__ void redo_dq_rows(uint32_t redo, int row0, const T* _
   }
 }
 // Key row j of dK and dV: dk_row[dh], dv_row[dh].  key(e) and value(e) are its elements, the key's scaled; `group` query heads read it, the
-// first at column 0 of q (rows ld apart) and d_o (rows h apart), row 0 of lse and delta (heads s apart); the last query row is `last`.
+// first at column 0 of q (rows ld apart) and d_o (rows h apart), row 0 of lse and delta (heads s apart); the last query row is `last`; delta stands there times `sign`.
 template <typename T, int SLOTS, int AHEAD, typename Key, typename Value>
 __device__ __forceinline__ void attention_key_row(Key key, Value value, const T* __restrict__ q, const T* __restrict__ d_o, int ld,
                                                   int h, const float* __restrict__ lse, const float* __restrict__ delta, int s,
-                                                  int group, int j, int last, int dh, int lane, float scale,
+                                                  int group, int j, int last, int dh, int lane, float scale, float sign,
                                                   T* __restrict__ dk_row, T* __restrict__ dv_row) {
   float dk[SLOTS], dv[SLOTS];
 #pragma unroll
@@ -212,7 +212,7 @@ __device__ __forceinline__ void attention_key_row(Key key, Value value, const T*
             dp = fmaf(value(e + u), to_f32(dr[e + u]), dp);
           }
         p = __expf(sc - lse[(size_t)g * s + i]);
-        ds = p * (dp - delta[(size_t)g * s + i]);
+        ds = p * (dp - sign * delta[(size_t)g * s + i]);
       }
       accumulate_weighted_rows<T, SLOTS, AHEAD>(dv, p, d0, h, n, dh, lane);
       accumulate_weighted_rows<T, SLOTS, AHEAD>(dk, ds, q0, ld, n, dh, lane);

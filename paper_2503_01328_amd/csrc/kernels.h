@@ -163,9 +163,6 @@ bool attention_backward(int dtype, const void* qkv, const void* o, const float* 
                         float* delta, void* partials, int s, int h, int n_heads, int n_kv_heads, bool force_generic,
                         hipStream_t stream);
 
-// delta[head][row] = dO . O of that row and head, rows of h = n_heads * 64 or 128 elements (attention_mfma.hip).
-bool attention_delta_bf16(const bf16* o, const bf16* d_o, float* delta, int rows, int h, int n_heads, hipStream_t stream);
-
 // ---- packed sequences (packed_plan.hip, attention_packed.hip, attention_packed_f32.hip, qk_norm_rotary.hip) ------------
 size_t packed_plan_bytes(int rows);  // 0: too many rows
 bool packed_plan(const int* lengths, int n, int rows, int* starts, int* positions, int* sequence, int* plan,

@@ -3,8 +3,9 @@
 //   [0] rows that sequences hold (`total`), [1] the row count the plan was made for, [2..15] unused
 //   first[padded]   first row of the row's sequence
 //   end[padded]     the row behind the last of the row's sequence
-//   key_order[blocks], query_order[blocks]   blocks of 128 rows, those that meet the most keys (queries) first, lower ones first
-//                                            among equals; blocks without a row of a sequence come last
+//   key_order[blocks][2], query_order[blocks][2]   blocks of 128 rows, those that meet the most tiles of 64 keys (queries) first, lower
+//                                                  ones first among equals, each with the first key that its rows see (the row behind
+//                                                  the last that sees its keys); blocks without a row of a sequence come last
 // padded: rows rounded up to whole blocks.  Rows behind the last sequence have first = rows (no key is visible to them) and
 // end = total (they are visible to no query, and both arrays never decrease).
 #pragma once
@@ -24,8 +25,8 @@ struct PackedPlan {
   __device__ __forceinline__ int total() const { return words[1] == rows ? words[0] : 0; }
   __host__ __device__ __forceinline__ const int* first() const { return words + kPlanHeader; }
   __host__ __device__ __forceinline__ const int* end() const { return first() + padded(); }
-  __host__ __device__ __forceinline__ const int* key_order() const { return end() + padded(); }
-  __host__ __device__ __forceinline__ const int* query_order() const { return key_order() + blocks(); }
+  __host__ __device__ __forceinline__ const int2* key_order() const { return reinterpret_cast<const int2*>(end() + padded()); }
+  __host__ __device__ __forceinline__ const int2* query_order() const { return key_order() + blocks(); }
 };
 
 }  // namespace po

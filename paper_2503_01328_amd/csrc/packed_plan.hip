@@ -3,8 +3,7 @@
 // (packed_plan.h).
 //
 // One launch.  Every block scans all lengths for itself (16384 of them are 64 KiB from the L2; a scan in a launch of its own would cost
-// more than repeating it) and keeps where each sequence ends in LDS; a thread then finds the sequence of the first of its four rows by
-// bisection and walks on from there.  The orders come from counting, for each block of 128 rows, the blocks that come before
+// more than repeating it) and keeps where each sequence ends in LDS; a thread then finds the sequence of its row by bisection.  The orders come from counting, for each block of 128 rows, the blocks that come before
 // it: the work of all of them stands in LDS too, a wave counts for one block at a time.
 // Sums of lengths stop at `rows`: a length below zero counts as zero, sequences that reach past the rows are cut there.
 #include "packed_plan.h"
@@ -13,7 +12,7 @@ namespace po {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kRowsPerThread = 4;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxSequences = 16384, kMaxRows = 1 << 21;  // 64 KiB of LDS each, for the ends and for the work of the blocks
 
 __device__ __forceinline__ int capped_sum(int a, int b, int cap) { return min(a + b, cap); }  // both at most 2^21
@@ -29,6 +28,15 @@ __device__ __forceinline__ int sequence_of(const int* ends, int n, int row) {
   return lo;
 }
 
+__device__ __forceinline__ int scan(int v, int lane, int cap) {  // inclusive, over the wave
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    if (lane >= o) v = capped_sum(v, u, cap);
+  }
+  return v;
+}
+
 }  // namespace
 
 __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __restrict__ lengths, int n, int rows,
@@ -41,21 +49,19 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __rest
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   // Each thread sums `per` lengths, the waves scan those sums, and every thread writes its ends.
+  for (int i = tid; i < n; i += kThreads) ends[i] = min(max(lengths[i], 0), rows);
+  __syncthreads();
   const int per = (n + kThreads - 1) / kThreads, from = min(tid * per, n), to = min(from + per, n);
   int sum = 0;
-  for (int i = from; i < to; ++i) sum = capped_sum(sum, min(max(lengths[i], 0), rows), rows);
-  int before = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(before, o, 64);
-    if (lane >= o) before = capped_sum(before, v, rows);
-  }
+  for (int i = from; i < to; ++i) sum = capped_sum(sum, ends[i], rows);
+  int before = scan(sum, lane, rows);
   if (lane == 63) wave_sums[wave] = before;
   before = __shfl_up(before, 1, 64);
   if (lane == 0) before = 0;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) before = capped_sum(before, wave_sums[w], rows);
-  for (int i = from; i < to; ++i) ends[i] = before = capped_sum(before, min(max(lengths[i], 0), rows), rows);
+  const int waves = scan(lane < kWaves ? wave_sums[lane] : 0, lane, rows);
+  if (wave > 0) before = capped_sum(before, __shfl(waves, wave - 1, 64), rows);
+  for (int i = from; i < to; ++i) ends[i] = before = capped_sum(before, ends[i], rows);
   __syncthreads();
 
   const int total = ends[n - 1];
@@ -64,30 +70,17 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __rest
 
   const PackedPlan p{plan, rows};
   const int blocks = p.blocks(), padded = p.padded();
-  const int row0 = (blockIdx.x * kThreads + tid) * kRowsPerThread;
-  if (row0 < padded) {
-    int j = row0 < total ? sequence_of(ends, n, row0) : 0, first[kRowsPerThread], end[kRowsPerThread];
-#pragma unroll
-    for (int u = 0; u < kRowsPerThread; ++u) {
-      const int row = row0 + u;
-      int seq = -1, pos = -1;
-      first[u] = rows;
-      end[u] = total;
-      if (row < total) {
-        while (ends[j] <= row) ++j;
-        first[u] = j ? ends[j - 1] : 0;
-        end[u] = ends[j];
-        seq = j;
-        pos = row - first[u];
-      }
-      if (row < rows) {
-        if (sequence) sequence[row] = seq;
-        if (positions) positions[row] = pos;
-      }
+  const int row = blockIdx.x * kThreads + tid;
+  if (row < padded) {
+    const bool held = row < total;
+    const int j = held ? sequence_of(ends, n, row) : -1, first = !held ? rows : j ? ends[j - 1] : 0;
+    if (row < rows) {
+      if (sequence) sequence[row] = j;
+      if (positions) positions[row] = held ? row - first : -1;
     }
     if (plan) {
-      *reinterpret_cast<int4*>(plan + kPlanHeader + row0) = make_int4(first[0], first[1], first[2], first[3]);
-      *reinterpret_cast<int4*>(plan + kPlanHeader + padded + row0) = make_int4(end[0], end[1], end[2], end[3]);
+      plan[kPlanHeader + row] = first;
+      plan[kPlanHeader + padded + row] = held ? ends[j] : total;
     }
   }
   if (!plan) return;
@@ -103,8 +96,8 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __rest
     work[b] = w;
   }
   __syncthreads();
-  int* key_order = plan + kPlanHeader + 2 * padded;
-  int* query_order = key_order + blocks;
+  int2* key_order = reinterpret_cast<int2*>(plan + kPlanHeader + 2 * padded);
+  int2* query_order = key_order + blocks;
   for (int b = blockIdx.x * kWaves + wave; b < blocks; b += gridDim.x * kWaves) {
     const unsigned mine = work[b], keys = mine >> 16, queries = mine & 0xffff;
     int k = 0, q = 0;
@@ -118,9 +111,10 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __rest
       k += __shfl_xor(k, o, 64);
       q += __shfl_xor(q, o, 64);
     }
-    if (lane == 0) {
-      key_order[k] = b;
-      query_order[q] = b;
+    if (lane < 2) {  // lane 0: the first row's sequence, lane 1: the last one's
+      const int r0 = b * kPlanBlock, r1 = min(r0 + kPlanBlock, total);
+      const int j = r0 < total ? sequence_of(ends, n, lane ? r1 - 1 : r0) : -1;
+      (lane ? query_order[q] : key_order[k]) = make_int2(b, j < 0 ? 0 : lane ? ends[j] : j ? ends[j - 1] : 0);
     }
   }
 }
@@ -128,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int* __rest
 size_t packed_plan_bytes(int rows) {
   if (rows <= 0 || rows > kMaxRows) return 0;
   const PackedPlan p{nullptr, rows};
-  return ((size_t)kPlanHeader + 2 * (size_t)p.padded() + 2 * (size_t)p.blocks()) * sizeof(int);
+  return ((size_t)kPlanHeader + 2 * (size_t)p.padded() + 4 * (size_t)p.blocks()) * sizeof(int);
 }
 
 bool packed_plan(const int* lengths, int n, int rows, int* starts, int* positions, int* sequence, int* plan,
@@ -142,7 +136,7 @@ bool packed_plan(const int* lengths, int n, int rows, int* starts, int* position
   const int smem = (n + kWaves + p.blocks()) * (int)sizeof(int);
   static LdsLimit lds;
   if (!lds.allow(packed_plan_kernel, (kMaxSequences + kWaves + kMaxRows / kPlanBlock) * (int)sizeof(int))) return false;
-  packed_plan_kernel<<<ceil_div(p.padded(), kThreads * kRowsPerThread), kThreads, smem, stream>>>(lengths, n, rows, starts,
+  packed_plan_kernel<<<ceil_div(p.padded(), kThreads), kThreads, smem, stream>>>(lengths, n, rows, starts,
                                                                                                  positions, sequence, plan);
   return launch_ok("packed_plan_kernel");
 }

@@ -69,8 +69,10 @@ def test_plan(gpu_device, lengths, rows):
     b1 = torch.clamp(b0 + 128, max=total)
     keys = torch.where(b0 < total, (b1 - first[b0] // 64 * 64 + 63) // 64, 0)
     queries = torch.where(b0 < total, (end[(b1 - 1).clamp(min=0)] - b0 + 63) // 64, 0)
-    for work, order in ((keys, plan[16 + 2 * padded:][:blocks]), (queries, plan[16 + 2 * padded + blocks:][:blocks])):
-        assert order.tolist() == sorted(range(blocks), key=lambda b: (-int(work[b]), b))
+    bounds = (torch.where(b0 < total, first[b0], 0), torch.where(b0 < total, end[(b1 - 1).clamp(min=0)], 0))
+    for work, bound, order in zip((keys, queries), bounds, plan[16 + 2 * padded:].reshape(2, blocks, 2)):
+        assert order[:, 0].tolist() == sorted(range(blocks), key=lambda b: (-int(work[b]), b))
+        assert torch.equal(order[:, 1].long(), bound[order[:, 0].long()].long())
 
 
 def test_plan_leaves_out_what_is_not_wanted(gpu_device):
@@ -91,17 +93,23 @@ def _inputs(dev, dtype, rows, h, hkv, seed, used=None):
     return qkv, d_o
 
 
-def _attention(dtype, qkv, d_o, plan, h, a, akv, o_in=None, lse_in=None):
+def _guarded(dev, dtype, *shape):
+    """A tensor of MARK in the middle of a buffer of it."""
+    n, edge = math.prod(shape), 1 << 16
+    whole = torch.full((n + 2 * edge,), MARK, dtype=dtype, device=dev)
+    return whole[edge:edge + n].view(shape), (whole[:edge], whole[edge + n:])
+
+
+def _attention(dtype, qkv, d_o, plan, h, a, akv):
     code, rows, dev = DT[dtype][0], qkv.shape[0], qkv.device
-    o = torch.full((rows, h), MARK, dtype=qkv.dtype, device=dev)
-    lse = torch.full((a, rows), MARK, device=dev)
-    dqkv = torch.full_like(qkv, MARK)
+    (o, edge_o), (lse, edge_lse), (dqkv, edge_d) = (_guarded(dev, t, *s) for t, s in ((qkv.dtype, (rows, h)), (torch.float32, (a, rows)),
+                                                                                 (qkv.dtype, qkv.shape)))
     po.po_op_attention_packed_forward(code, qkv, plan, o, lse, rows, h, a, akv)
     size = po.po_op_attention_packed_backward_workspace(code, rows, h, a, akv)
-    ws = torch.full((size + 64,), 255, dtype=torch.uint8, device=dev)  # NaN, and a margin to be left alone
-    po.po_op_attention_packed_backward(code, qkv, plan, o if o_in is None else o_in, lse if lse_in is None else lse_in, d_o, dqkv, ws, rows, h,
-                                       a, akv)
+    ws = torch.full((size + (1 << 16),), 255, dtype=torch.uint8, device=dev)  # NaN, and a margin to be left alone
+    po.po_op_attention_packed_backward(code, qkv, plan, o, lse, d_o, dqkv, ws, rows, h, a, akv)
     assert bool((ws[size:] == 255).all())
+    assert all(bool((t == MARK).all()) for edges in (edge_o, edge_lse, edge_d) for t in edges)
     return dict(o=o, lse=lse, dqkv=dqkv)
 
 
@@ -190,6 +198,28 @@ def test_attention_non_finite_rows_stay_in_their_sequence(gpu_device, dtype, dh,
         assert torch.isfinite(got[k][outside]).all()
     if where in "kv" and not math.isinf(value):
         assert got["o"][row, 3 if where == "v" else 0].isnan() and clean["o"][row].isfinite().all()
+
+
+@pytest.mark.parametrize("where", ["q", "k", "v", "d_o"])
+@pytest.mark.parametrize("dtype,dh,a,akv", [("f32", 64, 4, 2), ("bf16", 64, 4, 2), ("bf16", 128, 40, 8)])
+def test_attention_of_nan_sequences(gpu_device, dtype, dh, a, akv, where):
+    """A whole input NaN in one of three sequences: there everything that it reaches is NaN (dV of NaN values is not), elsewhere nothing."""
+    h, hkv, lengths, rows = a * dh, akv * dh, [400, 300, 500], 1200
+    qkv, d_o = _inputs(gpu_device, dtype, rows, h, hkv, 15)
+    want, tol = ref.attention(qkv, d_o, lengths, h, a, akv)
+    {"q": qkv[:, :h], "k": qkv[:, h:h + hkv], "v": qkv[:, h + hkv:], "d_o": d_o}[where][400:700] = math.nan
+    got = _attention(dtype, qkv, d_o, _plan(lengths, rows, gpu_device), h, a, akv)
+    inside = torch.zeros(rows, dtype=torch.bool, device=gpu_device)
+    inside[400:700] = True
+    for k in ("o", "lse", "dqkv"):
+        x, w, t = (y.T if k == "lse" else y for y in (got[k], want[k], tol[k]))
+        _within(x[~inside], w[~inside], t[~inside], k)
+    if where != "d_o":
+        assert got["o"][inside].isnan().all()
+    nan = got["dqkv"][inside].isnan()
+    assert nan[:, :h + hkv].all() and (where == "v" or nan[:, h + hkv:].all())
+    if where == "v":
+        _within(got["dqkv"][inside][:, h + hkv:], want["dqkv"][inside][:, h + hkv:], tol["dqkv"][inside][:, h + hkv:], "dV")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -18,8 +18,8 @@ def _refused(call, match, *args, **kw):
     assert e.value.code == po.PO_E_INVAL
 
 
-@pytest.mark.parametrize("rows,bytes_", [(0, 0), (-5, 0), (1, 4 * (16 + 256 + 2)), (128, 4 * (16 + 256 + 2)), (129, 4 * (16 + 512 + 4)),
-                                         (2097152, 4 * (16 + 2 * 2097152 + 2 * 16384)), (2097153, 0)])
+@pytest.mark.parametrize("rows,bytes_", [(0, 0), (-5, 0), (1, 4 * (16 + 256 + 4)), (128, 4 * (16 + 256 + 4)), (129, 4 * (16 + 512 + 8)),
+                                         (2097152, 4 * (16 + 2 * 2097152 + 4 * 16384)), (2097153, 0)])
 def test_plan_bytes(rows, bytes_):
     assert po.po_op_packed_plan_bytes(rows) == bytes_
 
