@@ -142,12 +142,8 @@ def po_last_error() -> str:
 
 
 def _ptr(t):
-    """Raw pointer of a torch tensor (device or host), an int, or None."""
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return C.c_void_p(t)
-    return C.c_void_p(t.data_ptr())
+    """Raw pointer of a torch tensor (device or host), an int, or None, for a void* parameter."""
+    return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
 def _stream(stream):

@@ -161,6 +161,24 @@ __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel
   if (redo) redo_packed_forward_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, o, h, hkv, group, head, scale);
 }
 
+// A tile's dS as the operands of dQ: rounded to bf16, and what that leaves rounded again, 16 bits in all.  dQ is the cheapest place to keep an error
+// down (a fragment of K feeds both MFMAs): with one term it was 1.53 to 1.62 times that of results computed in fp32 and rounded at the end, of which delta's
+// error, from the rounded o, is a third; with two it is 1.14 to 1.27, and the whole gradient 1.36 to 1.40 instead of 1.46 to 1.50.  Backward, us, one term
+// / two: 4096 rows, 32 heads of 128 over 8, 21 sequences 100 / 107; one sequence, 32 heads 450 / 502; 8192 rows, 40 heads of 64 over 8, 170 sequences 90 / 94.
+// The second term for dK or dV instead: 111 and 116, 498 and 498, 95 and 107.
+struct TwoTerms {
+  bf16x8 first[2], rest[2];
+  __device__ __forceinline__ explicit TwoTerms(f32x16 ds) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      first[st] = pack_bf16x8(ds, 8 * st);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ds[8 * st + e] -= (float)first[st][e];
+      rest[st] = pack_bf16x8(ds, 8 * st);
+    }
+  }
+};
+
 // 32 query rows of a head from q0 on.
 template <int DH>
 __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head, PackedPlan plan, int total,
@@ -213,7 +231,15 @@ __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head
         if (key > q || key < first) ds[e] = 0.f;
       }
     }
-    accumulate_tile<DH, false>(dq, ktile, ds, lane);
+    const TwoTerms w(ds);
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const bf16x8 k = read_tr_fragment<DH>(ktile, 16 * st, 32 * d, lane);
+        dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, w.rest[st], dq[d], 0, 0, 0);
+        dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, w.first[st], dq[d], 0, 0, 0);
+      }
     wait_lds_reads();
     if (t + F::NS * W < t_end) request(i, t + F::NS * W);
   }
@@ -660,11 +686,12 @@ __device__ __forceinline__ void packed_dq_block(char* smem, int q0, int key_firs
         for (int e = 0; e < 16; ++e)
           if ((unsigned)(rel + 8 * (e >> 2) + (e & 3)) > span) ds[e] = 0.f;
       }
-      const bf16x8 dsf[2] = {pack_bf16x8(ds, 0), pack_bf16x8(ds, 8)};
+      const TwoTerms w(ds);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < 2 * DT; ++m) {
-        dq[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], dsf[m / DT], dq[m % DT], 0, 0, 0);
+        dq[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], w.rest[m / DT], dq[m % DT], 0, 0, 0);
+        dq[m % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(2 * KS + m) % RING], w.first[m / DT], dq[m % DT], 0, 0, 0);
         if (m + RING < 2 * DT) ring[(2 * KS + m) % RING] = fragment(2 * KS + m + RING);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1049,11 +1076,9 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
   if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, h, n_heads, stream))
     return false;
   const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);
-  const bool few = (int64_t)n_heads * row_blocks <= std::min(32 * group, 128);
-  auto launch = h / n_heads == 64                       ? (few ? few_backward<64> : wide_backward<64, 2, 2>)
-                : few                                   ? few_backward<128>
-                : (int64_t)n_kv_heads * row_blocks <= 256 ? wide_backward<128, 2, 2>
-                                                        : wide_backward<128, 1, 3>;
+  const bool few = (int64_t)n_heads * row_blocks <= std::min(32 * group, 128), narrow = (int64_t)n_kv_heads * row_blocks <= 256;
+  auto launch = h / n_heads == 64 ? (few ? few_backward<64> : narrow ? wide_backward<64, 2, 2> : wide_backward<64, 1, 2>)
+                                  : (few ? few_backward<128> : narrow ? wide_backward<128, 2, 2> : wide_backward<128, 1, 3>);
   return launch((const bf16*)qkv, plan, lse, stats, (const bf16*)d_o, (bf16*)dqkv, rows, h, n_heads, n_kv_heads, stream);
 }
 
