@@ -20,7 +20,7 @@ namespace po {
 
 namespace {
 
-constexpr int kBlocks = 1024;  // of the backward at most: four on a CU; each leaves a partial sum of the gains' gradients
+constexpr int kBlocks = 1024;  // for queries and for keys at most in the backward; each leaves a partial sum of a gain's gradient
 constexpr int kMaxPairs = 128;
 
 struct Axes {
@@ -107,10 +107,10 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
                                                              float* __restrict__ partials, Shape s) {
   __shared__ float2 turns[4][kMaxPairs];
   __shared__ __align__(16) float gains[2 * LANES][16];  // for queries, for keys
-  __shared__ float sums[BACKWARD ? 4 : 1][BACKWARD ? 2 * 16 * LANES : 1];
+  __shared__ float sums[BACKWARD ? 4 : 1][BACKWARD ? 16 * LANES : 1];
   constexpr int HEADS = 64 / LANES;  // of a wave at a time
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (LANES - 1);
-  const int ld = s.h + 2 * s.hkv, heads = s.n_heads + s.n_kv_heads;
+  const int ld = s.h + 2 * s.hkv;
   const bool held = 16 * l < s.dh, rotated = 8 * l < s.pairs, norm = gain_q != nullptr;
   const int at_a = NEIGHBOURS || !rotated ? 16 * l : 8 * l, at_b = NEIGHBOURS || !rotated ? 16 * l + 8 : s.pairs + 8 * l;
   if (norm) {  // a lane's sixteen gains next to each other
@@ -125,11 +125,15 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
     }
     __syncthreads();
   }
-  float dq_a[8], dq_b[8], dk_a[8], dk_b[8];
+  float dg_a[8], dg_b[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dq_a[i] = dq_b[i] = dk_a[i] = dk_b[i] = 0.f;
+  for (int i = 0; i < 8; ++i) dg_a[i] = dg_b[i] = 0.f;
+  // Gradients of gains: the first half of the blocks takes the queries, the second the keys and values.
+  const bool parts = BACKWARD && norm;
+  const int blocks = parts ? gridDim.x / 2 : gridDim.x, part = (int)blockIdx.x >= blocks, block = blockIdx.x - part * blocks;
+  const int head_first = part ? s.n_heads : 0, head_end = parts && !part ? s.n_heads : s.n_heads + s.n_kv_heads;
 
-  for (int row = blockIdx.x * 4 + wave; row < s.rows; row += gridDim.x * 4) {
+  for (int row = block * 4 + wave; row < s.rows; row += blocks * 4) {
     if (positions[row] < 0) continue;  // no token there
     for (int p = lane; p < s.pairs; p += 64) {
       int axis = 0;
@@ -149,11 +153,11 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
       sn[i] = BACKWARD ? -cs.y : cs.y;
     }
     wave_sync();
-    for (int head0 = 0; head0 < heads; head0 += HEADS) {
+    for (int head0 = head_first; head0 < head_end; head0 += HEADS) {
       const int head = head0 + lane / LANES;
-      const bool mine = held && head < heads, is_q = head < s.n_heads;
+      const bool mine = held && head < head_end;
       const size_t at = (size_t)row * ld + (size_t)head * s.dh;
-      const float* gain = gains[(is_q ? 0 : LANES) + l];
+      const float* gain = gains[(head < s.n_heads ? 0 : LANES) + l];
       float a[8], b[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
@@ -188,15 +192,11 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
           }
           const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
           const float f = r * r * r * (sum_over_head<LANES>(dot) / (float)s.dh);
-          const float rq = is_q ? r : 0.f, rk = is_q ? 0.f : r;
           if (mine) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float ta = a[i] * x[i], tb = b[i] * y[i];
-              dq_a[i] = fmaf(ta, rq, dq_a[i]);
-              dq_b[i] = fmaf(tb, rq, dq_b[i]);
-              dk_a[i] = fmaf(ta, rk, dk_a[i]);
-              dk_b[i] = fmaf(tb, rk, dk_b[i]);
+              dg_a[i] = fmaf(a[i] * x[i], r, dg_a[i]);
+              dg_b[i] = fmaf(b[i] * y[i], r, dg_b[i]);
               a[i] = r * w[i] - x[i] * f;
               b[i] = r * z[i] - y[i] * f;
             }
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
       }
       if (mine) store_pairs<T, NEIGHBOURS>(out + at, at_a, at_b, a, b);
     }
-    if (in != out) {  // the values pass
+    if (in != out && (!parts || part)) {  // the values pass
       constexpr int V = Vec16<T>::N;
       const size_t v0 = (size_t)row * ld + s.h + s.hkv;
       for (int e = lane * V; e < s.hkv; e += 64 * V) store16(out + v0 + e, load16(in + v0 + e));
@@ -217,37 +217,34 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
     float* mine = sums[wave];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float v[4] = {dq_a[i], dq_b[i], dk_a[i], dk_b[i]};
+      float v[2] = {dg_a[i], dg_b[i]};
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int o = LANES; o < 64; o <<= 1) v[k] += __shfl_xor(v[k], o, 64);
       if (lane < LANES && held) {
-        const int ea = NEIGHBOURS ? 16 * l + 2 * i : at_a + i, eb = NEIGHBOURS ? 16 * l + 2 * i + 1 : at_b + i;
-        mine[ea] = v[0];
-        mine[eb] = v[1];
-        mine[s.dh + ea] = v[2];
-        mine[s.dh + eb] = v[3];
+        mine[NEIGHBOURS ? 16 * l + 2 * i : at_a + i] = v[0];
+        mine[NEIGHBOURS ? 16 * l + 2 * i + 1 : at_b + i] = v[1];
       }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * s.dh; e += 256)
-      partials[(size_t)blockIdx.x * 2 * s.dh + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+    for (int e = threadIdx.x; e < s.dh; e += 256)
+      partials[(size_t)blockIdx.x * s.dh + e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
   }
 }
 
-// dgain_q, dgain_k [dh] += the blocks' partial sums [blocks][2 dh]: a block eight columns, a thread every 32nd row of one (sixteen columns and every
+// dgain_q, dgain_k [dh] += the blocks' partial sums [2][blocks][dh]: a block eight columns, a thread every 32nd row of one (sixteen columns and every
 // sixteenth row took 25 us for 1024 rows, a load at a time).
 __global__ __launch_bounds__(256) void rotary_gain_sum_kernel(const float* __restrict__ partials, int blocks, int dh,
                                                               float* __restrict__ dgain_q, float* __restrict__ dgain_k) {
   __shared__ float sums[32][9];
-  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, e = blockIdx.x * 8 + x;  // 2 dh is a multiple of 8
-  const float* p = partials + e;
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3, e = blockIdx.x * 8 + x;  // dh is a multiple of 8
+  const float* p = partials + (e < dh ? e : (size_t)blocks * dh + e - dh);
   float v = 0.f;
   for (int b = y; b < blocks; b += 32 * 8) {
     float u[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] = b + 32 * k < blocks ? p[(size_t)(b + 32 * k) * 2 * dh] : 0.f;
+    for (int k = 0; k < 8; ++k) u[k] = b + 32 * k < blocks ? p[(size_t)(b + 32 * k) * dh] : 0.f;
     v += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
   }
   sums[y][x] = v;
@@ -351,7 +348,7 @@ bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out
     return false;
   }
   const int blocks = backward_blocks(a.rows);
-  launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, blocks, stream);
+  launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, a.gain_q ? 2 * blocks : ceil_div(a.rows, 4), stream);
   if (a.gain_q) rotary_gain_sum_kernel<<<2 * s.dh / 8, 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
   return launch_ok("qk_norm_rotary_kernel");
 }
