@@ -1058,8 +1058,9 @@ bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void*
 }
 
 size_t attention_packed_backward_workspace(int dtype, int rows, int h, int n_heads, int n_kv_heads) {
-  (void)h, (void)n_kv_heads;
-  return (size_t)n_heads * rows * sizeof(float) * (dtype == kBF16 ? 2 : 1);  // delta, and in bf16 the scaled lse
+  const size_t stats = (size_t)n_heads * rows;
+  // delta, and in bf16 the scaled lse; in fp32 partial results of dK and dV behind it, 16-byte aligned
+  return (dtype == kBF16 ? 2 * stats : (stats + 3) / 4 * 4 + attention_packed_f32_partials(rows, h, n_heads, n_kv_heads)) * sizeof(float);
 }
 
 bool attention_packed_backward(int dtype, const void* qkv, const int* plan, const void* o, const float* lse, const void* d_o,
@@ -1071,8 +1072,8 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
   float* stats = (float*)workspace;
   if (dtype == kF32)
     return attention_delta_f32((const float*)o, (const float*)d_o, stats, rows, h, n_heads, stream) &&
-           attention_packed_backward_f32((const float*)qkv, plan, lse, stats, (const float*)d_o, (float*)dqkv, rows, h, n_heads,
-                                         n_kv_heads, stream);
+           attention_packed_backward_f32((const float*)qkv, plan, lse, stats, (const float*)d_o, (float*)dqkv,
+                                         stats + ((size_t)n_heads * rows + 3) / 4 * 4, rows, h, n_heads, n_kv_heads, stream);
   if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, h, n_heads, stream))
     return false;
   const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);

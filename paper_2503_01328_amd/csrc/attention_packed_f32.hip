@@ -175,17 +175,18 @@ __device__ __forceinline__ void packed_f32_dq_block(float* lds, int q0, int head
   if (redo) redo_packed_dq_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, d_o, lse, delta, dqkv, h, hkv, group, head, scale, 1.f);
 }
 
-// 32 keys of a key/value head from k0 on; its waves walk the query tiles of every query head that reads it.
+// 32 keys from k0 on of the key/value head that `heads` query heads from head0 on read; its waves walk the query tiles of those.  `out`: column 0 of dK of
+// row 0, dV hkv columns further, rows ld_out apart.
 template <int DH>
-__device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int kv_head, PackedPlan plan, int total,
+__device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int head0, int heads, PackedPlan plan, int total,
                                                      const float* __restrict__ qkv, const float* __restrict__ d_o,
                                                      const float* __restrict__ lse, const float* __restrict__ delta,
-                                                     float* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+                                                     float* __restrict__ out, int ld_out, int h, int hkv, int group, float scale) {
   constexpr int DT = DH / 32, PART = kTileBytes<DH> / 4;  // a wave's tiles of Q and dO, later its partial results
   int lane = threadIdx.x & 63, half = lane >> 5, key = k0 + (lane & 31);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ld = h + 2 * hkv, last = total - 1, head0 = kv_head * group;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ld = h + 2 * hkv, last = total - 1, kv_head = head0 / group;
   const int end = plan.end()[key], end_lo = plan.end()[k0], end_hi = plan.end()[min(k0 + 31, last)];
-  const int t0 = k0 / 32, n_q = (end_hi - 1) / 32 + 1 - t0, n_it = group * n_q;
+  const int t0 = k0 / 32, n_q = (end_hi - 1) / 32 + 1 - t0, n_it = heads * n_q;
   const char* bytes = reinterpret_cast<const char*>(lds);
   const LaneReads<DH> reads(wave * 2 * PART * 4, lane);
   const unsigned q_lds = __builtin_amdgcn_readfirstlane((int)lds_byte(lds + wave * 2 * PART)), do_lds = q_lds + kTileBytes<DH>;
@@ -237,11 +238,10 @@ __device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int kv_
   const uint32_t bad_k = rows_to_redo(not_finite<DT>(dk), total - k0), bad_v = rows_to_redo(not_finite<DT>(dv), total - k0);
   if (lane == 0) redo_of[wave] = bad_k, redo_of[4 + wave] = bad_v;
   __syncthreads();
-  float* out = dqkv + h + kv_head * DH;
   const size_t stat_at = (size_t)head0 * plan.rows;
-  const uint32_t redo = keys_to_redo(all_redo(redo_of), all_redo(redo_of + 4), lse + stat_at, delta + stat_at, min(key, last), group, plan.rows);
+  const uint32_t redo = keys_to_redo(all_redo(redo_of), all_redo(redo_of + 4), lse + stat_at, delta + stat_at, min(key, last), heads, plan.rows);
   if (key <= last && !(redo >> (lane & 31) & 1)) {
-    float* to = out + (size_t)key * ld + 8 * wave + 4 * half;
+    float* to = out + (size_t)key * ld_out + 8 * wave + 4 * half;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       f32x4 vk, vv;
@@ -261,7 +261,7 @@ __device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int kv_
     }
   }
   if (redo)
-    redo_packed_key_rows<float, DH>(share_of(redo, wave), k0, plan, qkv, d_o, lse, delta, out, out + hkv, ld, h, hkv, group, group, head0,
+    redo_packed_key_rows<float, DH>(share_of(redo, wave), k0, plan, qkv, d_o, lse, delta, out, out + hkv, ld_out, h, hkv, group, heads, head0,
                                     scale, 1.f);
 }
 
@@ -270,25 +270,51 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void packed_f32_bwd_kernel(co
                                                                               const float* __restrict__ d_o,
                                                                               const float* __restrict__ lse,
                                                                               const float* __restrict__ delta, float* __restrict__ dqkv,
-                                                                              int rows, int h, int hkv, int group, float scale,
-                                                                              int dkv_blocks) {
+                                                                              float* __restrict__ partials, int heads, int rows, int h,
+                                                                              int hkv, int group, float scale, int dkv_blocks) {
   extern __shared__ __align__(16) float lds[];
   const PackedPlan plan{words, rows};
   const int total = plan.total();
   if (total == 0) return;
   const bool dkv = (int)blockIdx.x < dkv_blocks;
-  const int x = dkv ? blockIdx.x : blockIdx.x - dkv_blocks, n_x = dkv ? hkv / DH : h / DH, head = x % n_x, at = x / n_x;
+  const int x = dkv ? blockIdx.x : blockIdx.x - dkv_blocks, n_x = dkv ? h / DH / heads : h / DH, head = x % n_x, at = x / n_x;
   // of a block of 128 rows the first keys and the last queries meet the most
   const int row0 = dkv ? plan.query_order()[at >> 2].x * kPlanBlock + (at & 3) * 32
                        : plan.key_order()[at >> 2].x * kPlanBlock + (3 - (at & 3)) * 32;
   if (row0 >= total) return;
-  if (dkv)
-    packed_f32_dkv_block<DH>(lds, row0, head, plan, total, qkv, d_o, lse, delta, dqkv, h, hkv, group, scale);
-  else
+  if (dkv) {
+    const int head0 = head * heads, part = head0 % group / heads, column = head0 / group * DH;
+    float* out = partials ? partials + (size_t)part * rows * 2 * hkv + column : dqkv + h + column;
+    packed_f32_dkv_block<DH>(lds, row0, head0, heads, plan, total, qkv, d_o, lse, delta, out, partials ? 2 * hkv : h + 2 * hkv, h, hkv, group,
+                             scale);
+  } else
     packed_f32_dq_block<DH>(lds, row0, head, plan, total, qkv, d_o, lse, delta, dqkv, h, hkv, group, scale);
 }
 
+// dK and dV of every row of a sequence: the sum of the query heads' partial results [parts][rows][2 hkv], in their order.
+__global__ __launch_bounds__(256) void packed_f32_sum_kernel(const float* __restrict__ partials, const int* words, float* __restrict__ dqkv,
+                                                             int parts, int rows, int h, int hkv) {
+  const PackedPlan plan{words, rows};
+  const int per_row = hkv / 2;  // vectors
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= (size_t)plan.total() * per_row) return;
+  const size_t row = at / per_row, c = (at - row * per_row) * 4;
+  f32x4 v = *reinterpret_cast<const f32x4*>(partials + row * 2 * hkv + c);
+  for (int p = 1; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(partials + ((size_t)p * rows + row) * 2 * hkv + c);
+  *reinterpret_cast<f32x4*>(dqkv + row * (h + 2 * hkv) + h + c) = v;
+}
+
 // ---- host side -------------------------------------------------------------------------------------------------
+// Heads that share keys: a dK/dV block a query head, added up afterwards, while the blocks of whole groups, whose chains are that much longer, would fill
+// half of the CUs at most.  Backward, us, whole groups / by heads: 12 heads of 64 over 4, 1000 rows of 4 sequences (128 blocks) 61 / 45; 16 heads of
+// 128 over 4, 2000 rows (252) 263 / 272; 32 heads of 128 over 8, 2048 rows (512) 1184 / 1249.
+static bool by_heads(int rows, int n_heads, int n_kv_heads) {
+  return n_heads > n_kv_heads && (int64_t)n_kv_heads * ceil_div(rows, 32) <= 128;
+}
+size_t attention_packed_f32_partials(int rows, int h, int n_heads, int n_kv_heads) {
+  return by_heads(rows, n_heads, n_kv_heads) ? (size_t)rows * 2 * h : 0;  // group * 2 hkv columns
+}
+
 template <int DH>
 static bool forward_f32(const float* qkv, const int* plan, float* o, float* lse, int rows, int h, int n_heads, int n_kv_heads,
                         hipStream_t stream) {
@@ -301,14 +327,19 @@ static bool forward_f32(const float* qkv, const int* plan, float* o, float* lse,
 }
 
 template <int DH>
-static bool backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o, float* dqkv, int rows,
-                         int h, int n_heads, int n_kv_heads, hipStream_t stream) {
+static bool backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o, float* dqkv,
+                         float* partials, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream) {
   constexpr int smem = 8 * kTileBytes<DH> + 32;
   static LdsLimit lds;
   if (!lds.allow(packed_f32_bwd_kernel<DH>, smem)) return false;
-  const int tiles = ceil_div(rows, kPlanBlock) * 4;
-  packed_f32_bwd_kernel<DH><<<(n_kv_heads + n_heads) * tiles, 256, smem, stream>>>(
-      qkv, plan, d_o, lse, delta, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * tiles);
+  const int tiles = ceil_div(rows, kPlanBlock) * 4, group = n_heads / n_kv_heads, hkv = n_kv_heads * DH;
+  const bool split = by_heads(rows, n_heads, n_kv_heads);
+  const int heads = split ? 1 : group, dkv_blocks = n_heads / heads * tiles;
+  packed_f32_bwd_kernel<DH><<<dkv_blocks + n_heads * tiles, 256, smem, stream>>>(qkv, plan, d_o, lse, delta, dqkv, split ? partials : nullptr,
+                                                                                heads, rows, h, hkv, group, 1.0f / sqrtf((float)DH),
+                                                                                dkv_blocks);
+  if (split)
+    packed_f32_sum_kernel<<<(unsigned)(((size_t)rows * hkv / 2 + 255) / 256), 256, 0, stream>>>(partials, plan, dqkv, group, rows, h, hkv);
   return launch_ok("packed_f32_bwd_kernel");
 }
 
@@ -319,9 +350,9 @@ bool attention_packed_forward_f32(const float* qkv, const int* plan, float* o, f
 }
 
 bool attention_packed_backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o,
-                                   float* dqkv, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream) {
+                                   float* dqkv, float* partials, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream) {
   auto launch = h / n_heads == 128 ? backward_f32<128> : backward_f32<64>;
-  return launch(qkv, plan, lse, delta, d_o, dqkv, rows, h, n_heads, n_kv_heads, stream);
+  return launch(qkv, plan, lse, delta, d_o, dqkv, partials, rows, h, n_heads, n_kv_heads, stream);
 }
 
 }  // namespace po

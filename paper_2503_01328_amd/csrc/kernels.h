@@ -176,7 +176,8 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
 bool attention_packed_forward_f32(const float* qkv, const int* plan, float* o, float* lse, int rows, int h, int n_heads,
                                   int n_kv_heads, hipStream_t stream);
 bool attention_packed_backward_f32(const float* qkv, const int* plan, const float* lse, const float* delta, const float* d_o,
-                                   float* dqkv, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream);
+                                   float* dqkv, float* partials, int rows, int h, int n_heads, int n_kv_heads, hipStream_t stream);
+size_t attention_packed_f32_partials(int rows, int h, int n_heads, int n_kv_heads);  // floats
 constexpr int kMaxRotaryAxes = 4, kRotaryHalves = 0, kRotaryNeighbours = 1;
 struct QkNormRotary {
   const void *gain_q, *gain_k;  // [head size] of dtype; both null: no norm
