@@ -330,7 +330,7 @@ int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows,
  * d_o [rows, h], lse [n_heads, rows], dqkv like qkv, head sizes 64 and 128, all tensors 16-byte aligned.  plan: as po_op_packed_plan left it
  * for the same `rows` (of one made for another row count nothing is computed).  Rows behind the last sequence are not read as
  * keys or queries and left as they were in every output.  An infinity or NaN in a row of one sequence reaches no other sequence,
- * in a key or value row no row of o and dQ before it.  workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned,
+ * in a key or value row no row of o and dQ before it.  dqkv is neither qkv nor d_o.  workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned,
  * contents unspecified before and afterwards.  Results do not depend on how often or beside what a call runs: no atomics. */
 int po_op_attention_packed_forward(int32_t dtype, const void* qkv, const void* plan, void* o, float* lse, int32_t rows, int32_t h,
                                    int32_t n_heads, int32_t n_kv_heads, void* stream);
@@ -347,7 +347,7 @@ int po_op_attention_packed_backward(int32_t dtype, const void* qkv, const void* 
  * DEVICE int32 [n_axes, rows], n_axes 1 to 4, inv_freq DEVICE fp32; axis_pairs (HOST, [n_axes]) says how many pairs turn by each axis,
  * the first axis_pairs[0] by axis 0 and so on.  Together they are a multiple of 8 and at most half the head size; elements
  * behind them are not rotated.  Angles are formed in fp64.  A row whose position on axis 0 is negative holds nothing (positions of
- * po_op_packed_plan behind the last sequence) and is left as it was in out.  All tensors 16-byte aligned. */
+ * po_op_packed_plan behind the last sequence) and is left as it was in out.  All tensors 16-byte aligned, 1 to 2^25 rows. */
 int po_op_qk_norm_rotary_forward(int32_t dtype, const void* qkv, const void* gain_q, const void* gain_k, const int32_t* positions,
                                  const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes, int32_t layout, void* out,
                                  int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream);

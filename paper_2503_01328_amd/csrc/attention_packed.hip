@@ -1069,6 +1069,10 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
              (uintptr_t)qkv | (uintptr_t)o | (uintptr_t)d_o | (uintptr_t)dqkv | (uintptr_t)workspace,
              !qkv || !plan || !o || !lse || !d_o || !dqkv || !workspace, (uintptr_t)lse))
     return false;
+  if (dqkv == qkv || dqkv == d_o) {
+    set_error("attention_packed_backward: dqkv is another tensor than qkv and d_o");
+    return false;
+  }
   float* stats = (float*)workspace;
   if (dtype == kF32)
     return attention_delta_f32((const float*)o, (const float*)d_o, stats, rows, h, n_heads, stream) &&

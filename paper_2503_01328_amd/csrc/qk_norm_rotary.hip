@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kBlocks = 1024;  // for queries and for keys at most in the backward; each leaves a partial sum of a gain's gradient
 constexpr int kMaxPairs = 128;
+constexpr int kMaxRows = 1 << 25;  // a block of 256 threads for four of them: 2^31 threads
 
 struct Axes {
   int end[kMaxRotaryAxes];  // the pairs [end[i - 1], end[i]) turn by axis i
@@ -261,10 +262,10 @@ __global__ __launch_bounds__(256) void rotary_gain_sum_kernel(const float* __res
 
 bool check(const char* what, const QkNormRotary& a, const void* in, const void* x_in, const void* out, Axes& axes, Shape& s) {
   const int dh = a.n_heads > 0 ? a.h / a.n_heads : 0;
-  if (a.rows <= 0 || a.h <= 0 || a.n_heads <= 0 || a.h % a.n_heads != 0 || a.n_kv_heads <= 0 || a.n_heads % a.n_kv_heads != 0 ||
+  if (a.rows <= 0 || a.rows > kMaxRows || a.h <= 0 || a.n_heads <= 0 || a.h % a.n_heads != 0 || a.n_kv_heads <= 0 || a.n_heads % a.n_kv_heads != 0 ||
       dh % 16 != 0 || dh < 16 || dh > 256) {
-    set_error("%s: rows=%d h=%d heads=%d kv_heads=%d (head size h / heads a multiple of 16 up to 256, kv_heads a divisor of heads)",
-              what, a.rows, a.h, a.n_heads, a.n_kv_heads);
+    set_error("%s: rows=%d h=%d heads=%d kv_heads=%d (1 to %d rows, head size h / heads a multiple of 16 up to 256, kv_heads a divisor of "
+              "heads)", what, a.rows, a.h, a.n_heads, a.n_kv_heads, kMaxRows);
     return false;
   }
   if ((int64_t)a.h + 2 * (int64_t)a.n_kv_heads * dh > INT32_MAX) {

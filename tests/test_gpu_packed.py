@@ -134,8 +134,9 @@ def test_attention(gpu_device, dtype, dh, a, akv, lengths, rows):
 
 
 # launches that fill the chip, blocks that hold many sequences, and one that walks many tiles
-MANY = [("bf16", 128, 32, 8, [150] * 20 + [3] * 50, 3200), ("bf16", 64, 40, 40, [1000, 11, 2000], 3100), ("bf16", 128, 16, 2, [2500, 1, 90], 2600),
-        ("bf16", 128, 8, 8, [4096], 4096), ("bf16", 64, 40, 8, [37] * 100, 3712), ("bf16", 128, 40, 40, [600, 70, 1400], 2071), ("f32", 64, 16, 4, [900, 20, 400], 1400)]
+MANY = [("bf16", 64, 16, 4, [700, 1, 0, 900, 64], 1700), ("bf16", 64, 8, 8, [130] * 12, 1560), ("bf16", 128, 20, 4, [400, 33, 300], 800),
+        ("bf16", 128, 32, 8, [150] * 20 + [3] * 50, 3200), ("bf16", 64, 40, 40, [1000, 11, 2000], 3100), ("bf16", 128, 16, 2, [2500, 1, 90], 2600),
+        ("bf16", 128, 7, 7, [4096], 4096), ("bf16", 64, 40, 8, [37] * 100, 3712), ("bf16", 128, 40, 40, [600, 70, 1400], 2071), ("f32", 64, 16, 4, [900, 20, 400], 1400)]
 
 
 @pytest.mark.parametrize("dtype,dh,a,akv,lengths,rows", MANY, ids=lambda v: "" if isinstance(v, list) else str(v))
@@ -166,7 +167,8 @@ def test_attention_gradient_is_that_of_differences(gpu_device, dtype, dh):
 @pytest.mark.parametrize("where", ["q", "k", "v", "d_o"])
 @pytest.mark.parametrize("dtype,dh,a,akv,lengths", [("f32", 64, 2, 1, [10, 50, 20]), ("bf16", 64, 4, 2, [10, 50, 20]), ("f32", 128, 2, 2, [70, 90]),
                                                     ("bf16", 128, 2, 1, [33, 100, 200, 5]), ("bf16", 128, 32, 8, [300] * 10),
-                                                    ("bf16", 64, 40, 40, [300] * 10)])
+                                                    ("bf16", 64, 40, 40, [300] * 10), ("bf16", 64, 15, 15, [300] * 5),
+                                                    ("bf16", 128, 20, 4, [250] * 5)])
 def test_attention_non_finite_rows_stay_in_their_sequence(gpu_device, dtype, dh, a, akv, lengths, where, value):
     """One element that is not finite, in head 0 of a row in the middle of a sequence.  Every other sequence, and every other head, gets the
     results that it gets without; in key or value rows it reaches no row of o and dQ before it."""
@@ -360,7 +362,7 @@ def _rotary_case(dev, dtype, dh, a, akv, rows, axis_pairs, neighbours, norm, far
             _within(dg[i], start[i].double() + want[k], tol[k] + 2 * ref.E * (start[i].double().abs() + want[k].abs()), k)
 
 
-ROTARY = [(64, 4, 4, 1, [32], False, True), (64, 4, 2, 7, [32], True, True), (128, 16, 4, 100, [64], False, True), (128, 3, 1, 33, [16, 24, 24], False, True),
+ROTARY = [(64, 4, 4, 1, [32], False, True), (64, 4, 2, 7, [32], True, True), (128, 16, 8, 100, [64], False, True), (128, 3, 1, 33, [16, 24, 24], False, True),
           (128, 40, 8, 50, [10, 27, 27], True, True), (96, 6, 3, 40, [48], False, True), (96, 2, 1, 29, [9, 7, 8], True, False), (256, 4, 2, 21, [128], False, True),
           (256, 3, 3, 21, [30, 30, 30, 38], True, True), (32, 7, 7, 19, [16], False, True), (16, 5, 1, 11, [8], True, True), (48, 5, 5, 13, [16], False, True),
           (80, 2, 2, 12, [8, 16], False, True), (64, 40, 8, 65, [16], True, False), (64, 12, 4, 4200, [32], False, True), (128, 2, 2, 9, [0], False, True),
@@ -496,7 +498,7 @@ def test_a_layers_operators_together(gpu_device, dtype, rows, dh, a, akv, length
     layer.check()
 
 
-@pytest.mark.parametrize("dtype,rows,dh,a,akv", [("f32", 400, 64, 4, 2), ("bf16", 400, 64, 4, 2), ("bf16", 2048, 128, 16, 4)])
+@pytest.mark.parametrize("dtype,rows,dh,a,akv", [("f32", 400, 64, 4, 2), ("bf16", 400, 64, 4, 2), ("bf16", 2048, 128, 16, 8)])
 def test_captured_and_replayed_with_other_lengths(gpu_device, dtype, rows, dh, a, akv):
     """A graph of the whole run, replayed over new inputs and lengths, with eager runs of another batch between the replays."""
     layer, other = (_Layer(gpu_device, dtype, rows, dh, a, akv, [rows // 4] * 3, seed) for seed in (1, 2))

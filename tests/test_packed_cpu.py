@@ -62,6 +62,13 @@ def test_attention_refuses_pointers(dtype, call, names):
             _refused(f, "attention_packed", *args, stream=0)
 
 
+@pytest.mark.parametrize("dtype", [po.PO_F32, po.PO_BF16])
+@pytest.mark.parametrize("other", ["qkv", "d_o"])
+def test_attention_backward_refuses_its_inputs_as_output(dtype, other):
+    f, args = _backward(dtype, {**GOOD, "qkv": AT, "d_o": AT + 256, "dqkv": AT if other == "qkv" else AT + 256})
+    _refused(f, "another tensor", *args, stream=0)
+
+
 @pytest.mark.parametrize("call", [_forward, _backward])
 def test_attention_refuses_types(call):
     f, args = call(2, GOOD)
@@ -80,7 +87,7 @@ def test_workspaces():
 
 ROT = dict(qkv=AT, gain_q=AT, gain_k=AT, positions=AT, inv_freq=AT, axis_pairs=[32], layout=0, out=AT, d_out=AT, dqkv=AT + 64, dgain_q=AT, dgain_k=AT,
            workspace=AT, rows=10, h=256, n_heads=4, n_kv_heads=2, eps=1e-6)
-BAD_ROT = [dict(rows=0), dict(h=0), dict(n_heads=0), dict(n_heads=3), dict(n_kv_heads=3), dict(h=4 * 24), dict(h=4 * 8), dict(h=4 * 272),
+BAD_ROT = [dict(rows=0), dict(rows=2 ** 25 + 1), dict(h=0), dict(n_heads=0), dict(n_heads=3), dict(n_kv_heads=3), dict(h=4 * 24), dict(h=4 * 8), dict(h=4 * 272),
            dict(h=2 ** 30, n_heads=2 ** 22, n_kv_heads=2 ** 22), dict(axis_pairs=[]), dict(axis_pairs=[8] * 5), dict(axis_pairs=[36]), dict(axis_pairs=[40]),
            dict(axis_pairs=[12]), dict(axis_pairs=[40, -8]), dict(axis_pairs=[2 ** 31 - 1, 2 ** 31 - 1, 2]), dict(layout=2), dict(layout=-1), dict(eps=-1.0),
            dict(eps=math.nan), dict(eps=math.inf), dict(gain_q=None), dict(gain_k=None), dict(positions=None), dict(inv_freq=None), dict(gain_q=AT + 8),
