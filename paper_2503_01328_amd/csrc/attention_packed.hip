@@ -1,13 +1,27 @@
 // bf16 causal attention of packed sequences on the matrix cores, forward and backward: rows of many sequences back to back, row i sees
 // keys first(i) .. i, where first(i) is the first row of its sequence (packed_plan.h).
+//   O = softmax(Q K^T scale) V, lse = log of the softmax's sum; P = exp(S scale - lse), dP = dO V^T, delta = dO . O,
+//   dS = P (dP - delta), dQ = dS K scale, dK = dS^T Q scale, dV = P^T dO, the last two summed over the heads of a group.
 //
 // Blocks and tiles are cut from the packed axis, not from each sequence: a block of rows may hold the end of one sequence and several
 // whole ones, and walks the tiles from the first key that any of its rows sees to the diagonal.  That wastes no rows of a block on
-// short sequences, and the bounds first(i), end(j) of a row, one integer per lane, do all of the masking; tiles that every row sees whole pay
-// nothing for it.  Operand layouts are those of attention_mfma.hip.
+// short sequences, and the bounds first(i), end(j) of a row, one integer per lane, do all of the masking; tiles that every row sees
+// whole pay nothing for it.  Blocks start in the order of falling work, which the plan holds: the last to start are the shortest.
+// Operand layouts are those of attention_mfma.hip.
 //
-// P and dS are rounded to bf16 once on their way into the second product, as the inputs of every product here are; sums, maxima and
-// accumulators are fp32.
+// Three forms, by how much there is to share out (the rules stand at the entry points): "few", blocks of 32 rows whose eight (or four)
+// waves take a tile each; "wide" with SPLIT = 2, blocks of 64 rows by two pairs of waves that take half of the keys each; "wide" with
+// SPLIT = 1, blocks of 128 rows, 32 a wave, all waves against the same tiles.
+//
+// What bounds them: long sequences the matrix cores' issue (16384 rows in 3 sequences, 40 heads of 128: forward 1001 us, 967 TFLOP/s of
+// the 1135 that a large product reaches on this card; one sequence of 4096 rows, 32 heads of 128: forward 140 us, 980 TFLOP/s, backward
+// 504 us, 545 TFLOP/s, of which two terms of dS are 50 us); short ones what a block does besides its products: its place in the plan, first
+// tiles, masks and results, and the longest sequence's chain of tiles (4096 rows in 21 sequences, 32 heads of 128 over 8: 34 and 98 us; 8192
+// rows in 170, 40 heads of 64 over 8: 32 and 88; 2048 rows in 6, 16 heads of 128: 24 and 50).  Blocks of 32 rows alone took 2870 us for the
+// first of these and 88 and 188, 135 and 226, 31 and 84 for the last three.
+//
+// P and dS are rounded to bf16 once on their way into the second product, as the inputs of every product here are (dS for dQ in two
+// terms: TwoTerms); sums, maxima and accumulators are fp32.
 // A key or value that is not finite reaches the rows that see it and no other, nor does a row of d_o reach another sequence: results that
 // are not finite are redone row by row (attention_packed_rows.h).  Rows behind the last sequence read as zeros and are never written.
 #include <algorithm>
@@ -24,17 +38,24 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-// Waits for all loads in a way that the compiler sees.  It counts the loads of its own that may be outstanding (a kernel's rows, read into registers), cannot
-// see those requested by text, and would guard every use of such a register in the loop with a wait that is really one for the tiles under way.
+// Waits for all loads in a way that the compiler sees.  It counts the loads of its own that may be outstanding (a kernel's rows, read
+// into registers), cannot see those requested by text, and would guard every use of such a register in the loop with a wait that is
+// really one for the tiles under way: backward of 4096 rows, 32 heads of 128, 575 us so, 455 with one wait before the loop.
 __device__ __forceinline__ void wait_loads_visibly() {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), the other counters left alone (expcnt 7, lgkmcnt 15)
   asm volatile("" ::: "memory");
 }
 
+// ==================================================================================
+// Few blocks: 32 rows each, every wave with tiles and a ring of its own; merged through LDS at the end.
+// ==================================================================================
+
+// The running maximum and sum of a softmax, per row in lanes l and l + 32.  128 rows in 5 sequences, 8 heads of 64: 5.8 us, nearly all
+// of it latency (launch, plan, rows, tile, merge).
 template <int DH>
-__global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel(const bf16* __restrict__ qkv, const int* words,
-                                                                                bf16* __restrict__ o, float* __restrict__ lse,
-                                                                                int rows, int h, int hkv, int group, float scale) {
+__global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel(
+    const bf16* __restrict__ qkv, const int* words, bf16* __restrict__ o, float* __restrict__ lse, int rows, int h, int hkv, int group,
+    float scale) {
   using F = Few<DH, true>;
   constexpr int DT = DH / 32, W = F::W, PART = F::NS * F::STAGE / 4;
   extern __shared__ __align__(16) char smem[];
@@ -161,11 +182,12 @@ __global__ __launch_bounds__((64 * Few<DH, true>::W)) void packed_few_fwd_kernel
   if (redo) redo_packed_forward_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, o, h, hkv, group, head, scale);
 }
 
-// A tile's dS as the operands of dQ: rounded to bf16, and what that leaves rounded again, 16 bits in all.  dQ is the cheapest place to keep an error
-// down (a fragment of K feeds both MFMAs): with one term it was 1.53 to 1.62 times that of results computed in fp32 and rounded at the end, of which delta's
-// error, from the rounded o, is a third; with two it is 1.14 to 1.27, and the whole gradient 1.36 to 1.40 instead of 1.46 to 1.50.  Backward, us, one term
-// / two: 4096 rows, 32 heads of 128 over 8, 21 sequences 100 / 107; one sequence, 32 heads 450 / 502; 8192 rows, 40 heads of 64 over 8, 170 sequences 90 / 94.
-// The second term for dK or dV instead: 111 and 116, 498 and 498, 95 and 107.
+// A tile's dS as the operands of dQ: rounded to bf16, and what that leaves rounded again, 16 bits in all.  dQ is the cheapest place to
+// keep an error down (a fragment of K feeds both MFMAs): with one term it was 1.53 to 1.62 times that of results computed in fp32 and
+// rounded at the end, of which delta's error, from the rounded o, is a third; with two it is 1.14 to 1.27, and the whole gradient 1.36 to
+// 1.40 instead of 1.46 to 1.50.  Backward, us, one term / two: 4096 rows, 32 heads of 128 over 8, 21 sequences 100 / 107; one sequence,
+// 32 heads 450 / 502; 8192 rows, 40 heads of 64 over 8, 170 sequences 90 / 94.  The second term for dK or dV instead: 111 and 116, 498
+// and 498, 95 and 107.
 struct TwoTerms {
   bf16x8 first[2], rest[2];
   __device__ __forceinline__ explicit TwoTerms(f32x16 ds) {
@@ -183,9 +205,9 @@ struct TwoTerms {
 template <int DH>
 __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head, PackedPlan plan, int total,
                                                     const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                    const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
-                                                    bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+                                                    const float* __restrict__ lse, const float* __restrict__ from_lse,
+                                                    const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int h, int hkv,
+                                                    int group, float scale) {
   using F = Few<DH>;
   constexpr int DT = DH / 32, W = F::W, PART = F::NS * F::STAGE / 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -264,16 +286,17 @@ __device__ __forceinline__ void packed_few_dq_block(char* smem, int q0, int head
       store4(dqkv + (size_t)q * ld + head * DH + 8 * g + 4 * half, v);
     }
   }
-  if (redo) redo_packed_dq_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
+  if (redo)
+    redo_packed_dq_rows<bf16, DH>(share_of<W>(redo, wave), q0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
 }
 
 // 32 keys of a key/value head from k0 on; its waves walk the query tiles of every query head that reads it.
 template <int DH>
 __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_head, PackedPlan plan, int total,
                                                      const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                     const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
-                                                     bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+                                                     const float* __restrict__ lse, const float* __restrict__ from_lse,
+                                                     const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int h, int hkv,
+                                                     int group, float scale) {
   using F = Few<DH>;
   constexpr int DT = DH / 32, W = F::W, PART = F::NS * F::STAGE / 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -349,7 +372,8 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
   __syncthreads();
   bf16* out = dqkv + h + kv_head * DH;
   const size_t stat_at = (size_t)head0 * plan.rows;
-  const uint32_t redo = keys_to_redo(all_redo<W>(redo_of), all_redo<W>(redo_of + W), lse + stat_at, from_delta + stat_at, min(key, last), group, plan.rows);
+  const uint32_t redo = keys_to_redo(all_redo<W>(redo_of), all_redo<W>(redo_of + W), lse + stat_at, from_delta + stat_at,
+                                     min(key, last), group, plan.rows);
   if (key <= last && !(redo >> (lane & 31) & 1)) {
     bf16* to = out + (size_t)key * ld + 4 * half;
 #pragma unroll
@@ -376,11 +400,10 @@ __device__ __forceinline__ void packed_few_dkv_block(char* smem, int k0, int kv_
 }
 
 template <int DH>
-__global__ __launch_bounds__(64 * Few<DH>::W) void packed_few_bwd_kernel(const bf16* __restrict__ qkv, const int* words,
-                                                                        const bf16* __restrict__ d_o, const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv,
-                                                                        int rows, int h, int hkv, int group, float scale,
-                                                                        int dkv_blocks) {
+__global__ __launch_bounds__(64 * Few<DH>::W) void packed_few_bwd_kernel(
+    const bf16* __restrict__ qkv, const int* words, const bf16* __restrict__ d_o, const float* __restrict__ lse,
+    const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int rows, int h, int hkv, int group,
+    float scale, int dkv_blocks) {
   extern __shared__ __align__(16) char smem[];
   const PackedPlan plan{words, rows};
   const int total = plan.total();
@@ -401,8 +424,9 @@ __global__ __launch_bounds__(64 * Few<DH>::W) void packed_few_bwd_kernel(const b
 // Forward: four waves, each 32 rows against 32 keys at a time.
 // ==================================================================================
 
-// Consecutive blocks go to the eight XCDs in turn, each with an L2 of its own: heads that share keys and values go to the same one, next to
-// each other.
+// Consecutive blocks go to the eight XCDs in turn, each with an L2 of its own: heads that share keys and values go to the same one, next
+// to each other.  Forward of 16384 rows in 300 sequences, 40 heads of 128 over 8: 149 us by consecutive heads, 128 so; 4096 rows in 21, 32
+// heads, 36.2 and 33.4.
 __device__ __forceinline__ int head_of_block(int block, int n_heads, int group) {
   const int x = block % n_heads;
   return n_heads % 8 == 0 && group > 1 ? (x & 7) * (n_heads >> 3) + (x >> 3) : x;
@@ -426,10 +450,10 @@ struct BlockLoads {
   }
 };
 
-// Where a lane reads fragments in a tile of 32 rows, as LDS bytes from the tile on: row fragments (contraction over the head dimension), step kk: row lane % 32;
-// transposing ones (contraction over the rows), block d of 32 columns: rows 4 (lane / 32) + .., the second half 8 rows further.  A step
-// or block on is an XOR of the chunk's bits: of the KEEP first steps (half blocks) kept in a register each, of the others formed at every read; everything else
-// is a constant of the instruction.
+// Where a lane reads fragments in a tile of 32 rows, as LDS bytes from the tile on: row fragments (contraction over the head dimension),
+// step kk: row lane % 32; transposing ones (contraction over the rows), block d of 32 columns: rows 4 (lane / 32) + .., the second half 8
+// rows further.  A step or block on is an XOR of the chunk's bits: of the KEEP first steps (half blocks) kept in a register each, of the
+// others formed at every read; everything else is a constant of the instruction.
 template <int DH, int KEEP_ROW, int KEEP_COL>
 struct TileReads {
   int row[KEEP_ROW], col[KEEP_COL];
@@ -466,10 +490,13 @@ struct TileReads {
 };
 
 // SPLIT = 2: blocks of 64 rows, waves w and w + 2 own the same 32 and take one half of each stage's keys; merged through LDS at the end.
+// Stages of SUB tiles a wave, two in LDS (three measured the same).  A row's 2^S are taken against a reference that follows the maximum
+// only when that has outgrown it by 8: P stays below 2^8, the accumulators are rescaled in few tiles.  RING fragments are read ahead of
+// the MFMAs that take them, across the softmax, and hold the loop's reads in that order.
 template <int DH, int SPLIT, int SUB>
-__global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void packed_wide_fwd_kernel(const bf16* __restrict__ qkv, const int* words, bf16* __restrict__ o,
-                                                                  float* __restrict__ lse, int rows, int h, int hkv, int group,
-                                                                  float scale) {
+__global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void packed_wide_fwd_kernel(
+    const bf16* __restrict__ qkv, const int* words, bf16* __restrict__ o, float* __restrict__ lse, int rows, int h, int hkv, int group,
+    float scale) {
   constexpr int DT = DH / 32, KS = DH / 16, KT = 32 * SPLIT * SUB, BQ = 128 / SPLIT, TBYTES = KT * DH * 2, STAGE = 2 * TBYTES;
   constexpr int RING = DH == 64 ? 8 : 4;  // fragments read ahead
   using Loads = BlockLoads<DH, KT>;
@@ -613,18 +640,19 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void packed_wide_fwd_kernel
 }
 
 // ==================================================================================
-// Backward.  dQ blocks own rows, dK/dV blocks keys, 32 a wave; both form S and dP again:
-//   P = exp(S scale - lse), dS = P (dP - delta), dQ = dS K scale, dK = dS^T Q scale, dV = P^T dO.
+// Backward.  dQ blocks own rows, dK/dV blocks keys, 32 a wave; both form S and dP again, so that nothing is added up in memory and
+// results do not depend on an order.
 // ==================================================================================
 
-// 128 / SPLIT query rows of a head from q0 on, key0 the first key that they see.  SPLIT as in the forward.
+// 128 / SPLIT query rows of a head from q0 on, key_first the first key that they see.  SPLIT as in the forward, NST stages in LDS.
 template <int DH, int SPLIT, int NST>
 __device__ __forceinline__ void packed_dq_block(char* smem, int q0, int key_first, int head, PackedPlan plan, int total,
                                                 const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
-                                                bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
-  constexpr int DT = DH / 32, KS = DH / 16, KT = 32 * SPLIT, BQ = 128 / SPLIT, TBYTES = KT * DH * 2, STAGE = 2 * TBYTES, RING = DH == 128 ? 8 : 4;
+                                                const float* __restrict__ lse, const float* __restrict__ from_lse,
+                                                const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int h, int hkv, int group,
+                                                float scale) {
+  constexpr int DT = DH / 32, KS = DH / 16, KT = 32 * SPLIT, BQ = 128 / SPLIT, TBYTES = KT * DH * 2, STAGE = 2 * TBYTES;
+  constexpr int RING = DH == 128 ? 8 : 4;
   using Loads = BlockLoads<DH, KT>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int last = total - 1, ld = h + 2 * hkv, slice = wave / (4 / SPLIT);
@@ -731,8 +759,9 @@ __device__ __forceinline__ void packed_dq_block(char* smem, int q0, int key_firs
   if (redo) redo_packed_dq_rows<bf16, DH>(redo, qw0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
 }
 
-// 128 / SPLIT keys of a key/value head from k0 on, `end` the row behind the last that sees one of them; walks the query tiles of every head of the
-// group.  Heads of 128: the last V fragments stand in LDS, a place per lane, for want of registers.
+// 128 / SPLIT keys of a key/value head from k0 on, query_end the row behind the last that sees one of them; walks the query tiles of
+// every head of the group.  Heads of 128: the last V fragments stand in LDS, a place per lane, for want of registers (three where a
+// fourth would leave one block a CU).
 template <int DH, int SPLIT, int NST>
 struct KeyBlock {
   static constexpr int KT = 32 * SPLIT, TBYTES = KT * DH * 2, STATS = 4 * 256, STAGE = 2 * TBYTES + STATS;
@@ -741,9 +770,9 @@ struct KeyBlock {
 template <int DH, int SPLIT, int NST>
 __device__ __forceinline__ void packed_dkv_block(char* smem, int k0, int query_end, int kv_head, PackedPlan plan, int total,
                                                  const bf16* __restrict__ qkv, const bf16* __restrict__ d_o,
-                                                 const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta,
-                                                 bf16* __restrict__ dqkv, int h, int hkv, int group, float scale) {
+                                                 const float* __restrict__ lse, const float* __restrict__ from_lse,
+                                                 const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int h, int hkv, int group,
+                                                 float scale) {
   using B = KeyBlock<DH, SPLIT, NST>;
   constexpr int DT = DH / 32, KS = DH / 16, KT = B::KT, TBYTES = B::TBYTES, RING = 3, V_IN_REG = KS - B::V_IN_LDS;
   using Loads = BlockLoads<DH, KT>;
@@ -893,8 +922,8 @@ __device__ __forceinline__ void packed_dkv_block(char* smem, int k0, int query_e
   }
   bf16* out = dqkv + h + kv_head * DH;
   const size_t stat_at = (size_t)head0 * plan.rows;
-  const uint32_t redo = keys_to_redo(rows_to_redo(not_finite<DT>(dk), total - kw0), rows_to_redo(not_finite<DT>(dv), total - kw0), lse + stat_at,
-                                     from_delta + stat_at, min(key, last), group, plan.rows);
+  const uint32_t bad_k = rows_to_redo(not_finite<DT>(dk), total - kw0), bad_v = rows_to_redo(not_finite<DT>(dv), total - kw0);
+  const uint32_t redo = keys_to_redo(bad_k, bad_v, lse + stat_at, from_delta + stat_at, min(key, last), group, plan.rows);
   if (key <= last && !(redo >> (lane & 31) & 1)) {
     bf16* to = out + (size_t)key * ld + 4 * half;
 #pragma unroll
@@ -917,22 +946,24 @@ __device__ __forceinline__ void packed_dkv_block(char* smem, int k0, int query_e
 }
 
 template <int DH, int SPLIT, int NST>
-__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_wide_bwd_kernel(const bf16* __restrict__ qkv, const int* words,
-                                                                  const bf16* __restrict__ d_o, const float* __restrict__ lse,
-                                                     const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int rows,
-                                                                  int h, int hkv, int group, float scale, int dkv_blocks) {
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_wide_bwd_kernel(
+    const bf16* __restrict__ qkv, const int* words, const bf16* __restrict__ d_o, const float* __restrict__ lse,
+    const float* __restrict__ from_lse, const float* __restrict__ from_delta, bf16* __restrict__ dqkv, int rows, int h, int hkv, int group,
+    float scale, int dkv_blocks) {
   extern __shared__ __align__(16) char smem[];
   const PackedPlan plan{words, rows};
   const int total = plan.total();
   if (total == 0) return;
-  // dK/dV blocks first: the dQ blocks start on the CUs that light ones leave early
+  // dK/dV blocks first, as one of them does up to a group's heads more: the dQ blocks start on the CUs that light ones leave early
+  // (4096 rows in 21 sequences, 32 heads of 128 over 8: 105 us, the other way round 117)
   if ((int)blockIdx.x < dkv_blocks) {
     const int n_kv = hkv / DH, at = blockIdx.x / n_kv;
     const int2 block = plan.query_order()[at / SPLIT];
     const int k0 = block.x * kPlanBlock + at % SPLIT * (128 / SPLIT);
     if (k0 >= total) return;
     const int end = SPLIT == 1 ? block.y : plan.end()[min(k0 + 128 / SPLIT, total) - 1];
-    packed_dkv_block<DH, SPLIT, NST>(smem, k0, end, blockIdx.x % n_kv, plan, total, qkv, d_o, lse, from_lse, from_delta, dqkv, h, hkv, group, scale);
+    packed_dkv_block<DH, SPLIT, NST>(smem, k0, end, blockIdx.x % n_kv, plan, total, qkv, d_o, lse, from_lse, from_delta, dqkv, h, hkv,
+                                     group, scale);
   } else {
     const int x = blockIdx.x - dkv_blocks, n_heads = h / DH, at = x / n_heads;
     const int2 block = plan.key_order()[at / SPLIT];
@@ -944,7 +975,8 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_wide_bwd_kernel
 }
 
 // What the backward adds to scores and to dP, as the initial value of their accumulators: from_lse = -lse / scale and from_delta = -delta,
-// delta = dO . O of a row and head; DH / 8 lanes a row and head, 16 bytes of both per lane.
+// delta = dO . O of a row and head; DH / 8 lanes a row and head, 16 bytes of both per lane.  Bound
+// by memory: 4096 rows, 32 heads of 128, 67 MB, 13.6 us; 8192 rows, 40 heads of 64, 84 MB, 20.4 us.
 template <int DH>
 __global__ __launch_bounds__(256) void packed_stats_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o,
                                                            const float* __restrict__ lse, float* __restrict__ from_lse,
@@ -978,15 +1010,18 @@ static bool statistics(const bf16* o, const bf16* d_o, const float* lse, float* 
 template <int DH, int SPLIT, int NST>
 static bool wide_backward(const bf16* qkv, const int* plan, const float* lse, const float* stats, const bf16* d_o, bf16* dqkv, int rows,
                            int h, int n_heads, int n_kv_heads, hipStream_t stream) {
-  constexpr int dq = NST * 2 * 32 * SPLIT * DH * 2, dkv = KeyBlock<DH, SPLIT, NST>::BYTES, merge = SPLIT == 2 ? 4 * 64 * (DH / 32) * 16 * 4 : 0;
+  constexpr int dq = NST * 2 * 32 * SPLIT * DH * 2, dkv = KeyBlock<DH, SPLIT, NST>::BYTES;
+  constexpr int merge = SPLIT == 2 ? 4 * 64 * (DH / 32) * 16 * 4 : 0;
   constexpr int smem = dkv > merge ? (dkv > dq ? dkv : dq) : (merge > dq ? merge : dq);
   static LdsLimit lds;
   if (!lds.allow(packed_wide_bwd_kernel<DH, SPLIT, NST>, smem)) return false;
   const int blocks = ceil_div(rows, kPlanBlock) * SPLIT;
   packed_wide_bwd_kernel<DH, SPLIT, NST><<<(n_kv_heads + n_heads) * blocks, 256, smem, stream>>>(
-      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * blocks);
+      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads,
+      1.0f / sqrtf((float)DH), n_kv_heads * blocks);
   return launch_ok("packed_wide_bwd_kernel");
 }
+
 template <int DH, int SPLIT, int SUB>
 static bool wide_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, int rows, int h, int n_heads, int n_kv_heads,
                           hipStream_t stream) {
@@ -997,6 +1032,7 @@ static bool wide_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, 
       qkv, plan, o, lse, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH));
   return launch_ok("packed_wide_fwd_kernel");
 }
+
 template <int DH>
 static bool few_forward(const bf16* qkv, const int* plan, bf16* o, float* lse, int rows, int h, int n_heads, int n_kv_heads,
                         hipStream_t stream) {
@@ -1018,7 +1054,8 @@ static bool few_backward(const bf16* qkv, const int* plan, const float* lse, con
   if (!lds.allow(packed_few_bwd_kernel<DH>, smem)) return false;
   const int tiles = ceil_div(rows, kPlanBlock) * 4;
   packed_few_bwd_kernel<DH><<<(n_kv_heads + n_heads) * tiles, 64 * F::W, smem, stream>>>(
-      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads, 1.0f / sqrtf((float)DH), n_kv_heads * tiles);
+      qkv, plan, d_o, lse, stats, stats + (size_t)n_heads * rows, dqkv, rows, h, n_kv_heads * DH, n_heads / n_kv_heads,
+      1.0f / sqrtf((float)DH), n_kv_heads * tiles);
   return launch_ok("packed_few_bwd_kernel");
 }
 
@@ -1051,6 +1088,11 @@ bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void*
     return false;
   if (dtype == kF32)
     return attention_packed_forward_f32((const float*)qkv, plan, (float*)o, lse, rows, h, n_heads, n_kv_heads, stream);
+  // Larger blocks share more of each tile, smaller ones fill more of the 256 CUs and leave shorter chains behind a long sequence.  Forward,
+  // us, few / 64 rows / 128 rows, by heads x blocks of 128 rows; in brackets one sequence, before it 50 to 100:
+  //   heads of 64:   64: 5.9 6.5 7.8 [12.6 23.5 35.7];  128: 9.8 6.7 8.3 [10 sequences 12.8 12.2 18.1];  512: - 11.0 10.2 [- 54 71];
+  //   640: - 16.3 14.2 [- 37 40].   128: 64: 8.0 9.3 10.8;  128: 13.5 9.4 11.8;  256: - 12.6 12.2 [- 36 51];  320: - 18.5 15.5 [2
+  //   sequences - 23.0 24.2];  512: - 23.0 17.4 [- 92 103].
   const int64_t blocks = (int64_t)n_heads * ceil_div(rows, kPlanBlock);
   auto launch = h / n_heads == 128 ? (blocks <= 64 ? few_forward<128> : blocks <= 384 ? wide_forward<128, 2, 1> : wide_forward<128, 1, 1>)
                                    : (blocks <= 64 ? few_forward<64> : blocks <= 512 ? wide_forward<64, 2, 1> : wide_forward<64, 1, 2>);
@@ -1081,6 +1123,12 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
   if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, h, n_heads, stream))
     return false;
   const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);
+  // As in the forward; blocks of keys are n_kv_heads x row_blocks and each walks its whole group.  Backward, us:
+  //   few / 64 rows, by n_heads x row_blocks: heads of 128, no groups 32: 12.6 14.4, 64: 18.5 15.1; groups of 4, 128: 26.0 29.9 and, fewer
+  //   and longer sequences, 39.6 63.4; 256: 46.3 32.8 and 61.9 75.5.
+  //   64 rows / 128 rows, by n_kv_heads x row_blocks: heads of 128, 256: 16 heads, 5 sequences 40.8 47.1, one 77 97; 32 heads over 8, 10
+  //   sequences 125 156; 512: 32 over 8, 204 sequences 148 126, 20 sequences 251 226.  Heads of 64, 256: 40 over 8, 10 sequences 87 140;
+  //   16 heads, 5 sequences 23.6 32; 512: 40 over 8, 170 sequences 100 90; 640: 40 heads 42 37; 1024: 32 heads, one sequence 283 275.
   const bool few = (int64_t)n_heads * row_blocks <= std::min(32 * group, 128), narrow = (int64_t)n_kv_heads * row_blocks <= 256;
   auto launch = h / n_heads == 64 ? (few ? few_backward<64> : narrow ? wide_backward<64, 2, 2> : wide_backward<64, 1, 2>)
                                   : (few ? few_backward<128> : narrow ? wide_backward<128, 2, 2> : wide_backward<128, 1, 3>);

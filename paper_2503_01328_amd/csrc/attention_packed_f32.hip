@@ -1,9 +1,11 @@
 // fp32 causal attention of packed sequences on the matrix cores (full fp32 products and sums), forward and backward.
 //
 // Masks and block order are those of attention_packed.hip, tiles, operand layouts and the four waves that split a block's tiles those of
-// attention_f32.hip: a block owns 32 rows, wave w takes every fourth tile and reads its own copy of it, partial results are added in wave order.
-// Eight waves for heads of 64, which LDS has room for, gain where chains of tiles are long for the launch (12 heads over 4, 1000 rows, backward 61.1 -> 55.9 us) and lose
-// elsewhere (16 heads, 4000 rows of 60 sequences 111 -> 158, 32 heads, 3000 rows 1090 -> 1176).
+// attention_f32.hip: a block owns 32 rows, wave w takes every fourth tile and reads its own copy of it, partial results are added in wave
+// order.  Bound by the chain of tiles of the longest sequence while the launch does not fill the chip: 12 heads of 64 over 4, 1000 rows of
+// 4 sequences, forward 22 us, backward 54 with its sums, against 13 us of products at the rate of a large one.
+// Eight waves for heads of 64, which LDS has room for, gain where chains of tiles are long for the launch (this shape's backward with
+// whole groups 61.1 -> 55.9 us) and lose elsewhere (16 heads, 4000 rows of 60 sequences 111 -> 158, 32 heads, 3000 rows 1090 -> 1176).
 #include "attention_f32_tile.h"
 #include "attention_packed_rows.h"
 
@@ -175,8 +177,8 @@ __device__ __forceinline__ void packed_f32_dq_block(float* lds, int q0, int head
   if (redo) redo_packed_dq_rows<float, DH>(share_of(redo, wave), q0, plan, qkv, d_o, lse, delta, dqkv, h, hkv, group, head, scale, 1.f);
 }
 
-// 32 keys from k0 on of the key/value head that `heads` query heads from head0 on read; its waves walk the query tiles of those.  `out`: column 0 of dK of
-// row 0, dV hkv columns further, rows ld_out apart.
+// 32 keys from k0 on of the key/value head that `heads` query heads from head0 on read; its waves walk the query tiles of those.  `out`:
+// column 0 of dK of row 0, dV hkv columns further, rows ld_out apart.
 template <int DH>
 __device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int head0, int heads, PackedPlan plan, int total,
                                                      const float* __restrict__ qkv, const float* __restrict__ d_o,
@@ -239,7 +241,8 @@ __device__ __forceinline__ void packed_f32_dkv_block(float* lds, int k0, int hea
   if (lane == 0) redo_of[wave] = bad_k, redo_of[4 + wave] = bad_v;
   __syncthreads();
   const size_t stat_at = (size_t)head0 * plan.rows;
-  const uint32_t redo = keys_to_redo(all_redo(redo_of), all_redo(redo_of + 4), lse + stat_at, delta + stat_at, min(key, last), heads, plan.rows);
+  const uint32_t redo = keys_to_redo(all_redo(redo_of), all_redo(redo_of + 4), lse + stat_at,
+                                     delta + stat_at, min(key, last), heads, plan.rows);
   if (key <= last && !(redo >> (lane & 31) & 1)) {
     float* to = out + (size_t)key * ld_out + 8 * wave + 4 * half;
 #pragma unroll
@@ -305,9 +308,9 @@ __global__ __launch_bounds__(256) void packed_f32_sum_kernel(const float* __rest
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------
-// Heads that share keys: a dK/dV block a query head, added up afterwards, while the blocks of whole groups, whose chains are that much longer, would fill
-// half of the CUs at most.  Backward, us, whole groups / by heads: 12 heads of 64 over 4, 1000 rows of 4 sequences (128 blocks) 61 / 45; 16 heads of
-// 128 over 4, 2000 rows (252) 263 / 272; 32 heads of 128 over 8, 2048 rows (512) 1184 / 1249.
+// Heads that share keys: a dK/dV block a query head, added up afterwards, while the blocks of whole groups, whose chains are that much
+// longer, would fill half of the CUs at most.  Backward, us, whole groups / by heads: 12 heads of 64 over 4, 1000 rows of 4 sequences (128
+// blocks) 61 / 45; 16 heads of 128 over 4, 2000 rows (252) 263 / 272; 32 heads of 128 over 8, 2048 rows (512) 1184 / 1249.
 static bool by_heads(int rows, int n_heads, int n_kv_heads) {
   return n_heads > n_kv_heads && (int64_t)n_kv_heads * ceil_div(rows, 32) <= 128;
 }

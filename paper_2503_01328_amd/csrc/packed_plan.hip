@@ -3,8 +3,10 @@
 // (packed_plan.h).
 //
 // One launch.  Every block scans all lengths for itself (16384 of them are 64 KiB from the L2; a scan in a launch of its own would cost
-// more than repeating it) and keeps where each sequence ends in LDS; a thread then finds the sequence of its row by bisection.  The orders come from counting, for each block of 128 rows, the blocks that come before
-// it: the work of all of them stands in LDS too, a wave counts for one block at a time.
+// more than repeating it) and keeps where each sequence ends in LDS; a thread then finds the sequence of its row by bisection.  The orders
+// come from counting, for each block of 128 rows, the blocks that come before it: the work of all of them stands in LDS too, a wave counts
+// for one block at a time.
+// Bound by latency, of the launch, the scan and the bisections: 2048 rows in 8 sequences 4.8 us, 131072 rows in 4000 10.8.
 // Sums of lengths stop at `rows`: a length below zero counts as zero, sequences that reach past the rows are cut there.
 #include "packed_plan.h"
 
@@ -136,8 +138,7 @@ bool packed_plan(const int* lengths, int n, int rows, int* starts, int* position
   const int smem = (n + kWaves + p.blocks()) * (int)sizeof(int);
   static LdsLimit lds;
   if (!lds.allow(packed_plan_kernel, (kMaxSequences + kWaves + kMaxRows / kPlanBlock) * (int)sizeof(int))) return false;
-  packed_plan_kernel<<<ceil_div(p.padded(), kThreads), kThreads, smem, stream>>>(lengths, n, rows, starts,
-                                                                                                 positions, sequence, plan);
+  packed_plan_kernel<<<ceil_div(p.padded(), kThreads), kThreads, smem, stream>>>(lengths, n, rows, starts, positions, sequence, plan);
   return launch_ok("packed_plan_kernel");
 }
 
