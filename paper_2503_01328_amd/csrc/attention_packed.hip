@@ -975,35 +975,48 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void packed_wide_bwd_kernel
 }
 
 // What the backward adds to scores and to dP, as the initial value of their accumulators: from_lse = -lse / scale and from_delta = -delta,
-// delta = dO . O of a row and head; DH / 8 lanes a row and head, 16 bytes of both per lane.  Bound
-// by memory: 4096 rows, 32 heads of 128, 67 MB, 13.6 us; 8192 rows, 40 heads of 64, 84 MB, 20.4 us.
+// delta = dO . O of a row and head.  Bound by memory.  A block takes 32 rows of a head, DH / 8 lanes a row with 16 bytes of both each, all
+// asked for before the first is used, and writes their values next to each other: 8192 rows, 40 heads of 64, the whole backward 94 us with
+// a row of all heads after the other, whose results go to as many places as there are heads, 87 so (two to eight heads a block the same).
+constexpr int kStatRows = 32;
 template <int DH>
 __global__ __launch_bounds__(256) void packed_stats_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o,
                                                            const float* __restrict__ lse, float* __restrict__ from_lse,
-                                                           float* __restrict__ from_delta, int rows, int h, float to_lse) {
-  constexpr int LANES = DH / 8;
-  const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x, pair = t / LANES;
-  const unsigned n_heads = h / DH, row = (unsigned)(pair / n_heads), head = (unsigned)(pair - (size_t)row * n_heads);
-  float d = 0.f;
-  if (row < (unsigned)rows) {
-    const bf16x8 a = *reinterpret_cast<const bf16x8*>(o + t * 8), b = *reinterpret_cast<const bf16x8*>(d_o + t * 8);
+                                                           float* __restrict__ from_delta, int rows, int n_heads, float to_lse) {
+  constexpr int LANES = DH / 8, STEP = 256 / LANES, N = kStatRows / STEP;
+  __shared__ float sums[kStatRows];
+  const int head = blockIdx.x % n_heads, row0 = blockIdx.x / n_heads * kStatRows;
+  const int mine = threadIdx.x / LANES, e = threadIdx.x % LANES * 8;
+  bf16x8 a[N], b[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d = fmaf((float)a[e], (float)b[e], d);
+  for (int i = 0; i < N; ++i) {
+    const size_t at = ((size_t)min(row0 + mine + i * STEP, rows - 1) * n_heads + head) * DH + e;
+    a[i] = *reinterpret_cast<const bf16x8*>(o + at);
+    b[i] = *reinterpret_cast<const bf16x8*>(d_o + at);
   }
 #pragma unroll
-  for (int m = 1; m < LANES; m <<= 1) d += __shfl_xor(d, m);
-  if (row < (unsigned)rows && threadIdx.x % LANES == 0) {
+  for (int i = 0; i < N; ++i) {
+    float d = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d = fmaf((float)a[i][j], (float)b[i][j], d);
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) d += __shfl_xor(d, m);
+    if (e == 0) sums[mine + i * STEP] = d;
+  }
+  __syncthreads();
+  const int row = row0 + threadIdx.x;
+  if (threadIdx.x < kStatRows && row < rows) {
     const size_t at = (size_t)head * rows + row;
     from_lse[at] = lse[at] * to_lse;
-    from_delta[at] = -d;
+    from_delta[at] = -sums[threadIdx.x];
   }
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------
 template <int DH>
-static bool statistics(const bf16* o, const bf16* d_o, const float* lse, float* stats, int rows, int h, int n_heads, hipStream_t stream) {
-  packed_stats_kernel<DH><<<(unsigned)(((size_t)rows * h / 8 + 255) / 256), 256, 0, stream>>>(
-      o, d_o, lse, stats, stats + (size_t)n_heads * rows, rows, h, -sqrtf((float)DH));
+static bool statistics(const bf16* o, const bf16* d_o, const float* lse, float* stats, int rows, int n_heads, hipStream_t stream) {
+  packed_stats_kernel<DH><<<n_heads * ceil_div(rows, kStatRows), 256, 0, stream>>>(o, d_o, lse, stats, stats + (size_t)n_heads * rows,
+                                                                                  rows, n_heads, -sqrtf((float)DH));
   return launch_ok("packed_stats_kernel");
 }
 
@@ -1120,7 +1133,7 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
     return attention_delta_f32((const float*)o, (const float*)d_o, stats, rows, h, n_heads, stream) &&
            attention_packed_backward_f32((const float*)qkv, plan, lse, stats, (const float*)d_o, (float*)dqkv,
                                          stats + ((size_t)n_heads * rows + 3) / 4 * 4, rows, h, n_heads, n_kv_heads, stream);
-  if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, h, n_heads, stream))
+  if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, n_heads, stream))
     return false;
   const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);
   // As in the forward; blocks of keys are n_kv_heads x row_blocks and each walks its whole group.  Backward, us:
