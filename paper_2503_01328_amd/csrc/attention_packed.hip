@@ -489,6 +489,29 @@ struct TileReads {
   }
 };
 
+// A row's columns 16 k + 8 b + 4 half + 0 .. 3 of a result, b = 0 in v0 and 1 in v1, to `to` = column 16 k.  The half-waves exchange half of
+// theirs, so that a lane writes 16 bytes, not twice 8: forward and backward of 16384 rows in 300 sequences, 40 heads of 128 over 8, 127 and
+// 350 us so far, 111 and 328 with it; 2048 rows in 6, 16 heads of 128, backward 42 and 38.  Whole lines, by more exchanges, took the same.
+__device__ __forceinline__ void store_pair(bf16* to, const f32x4& v0, const f32x4& v1, int half) {
+  union {
+    bf16x4 v;
+    unsigned u[2];
+  } a, b;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) a.v[r] = (bf16)v0[r], b.v[r] = (bf16)v1[r];
+  union {
+    unsigned u[4];
+    bf16x8 v;
+  } x;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {  // the upper half of a against the lower half of b
+    const auto swapped = __builtin_amdgcn_permlane32_swap(a.u[r], b.u[r], false, false);
+    x.u[r] = swapped[0];
+    x.u[2 + r] = swapped[1];
+  }
+  *reinterpret_cast<bf16x8*>(to + 8 * half) = x.v;
+}
+
 // SPLIT = 2: blocks of 64 rows, waves w and w + 2 own the same 32 and take one half of each stage's keys; merged through LDS at the end.
 // Stages of SUB tiles a wave, two in LDS (three measured the same).  A row's 2^S are taken against a reference that follows the maximum
 // only when that has outgrown it by 8: P stays below 2^8, the accumulators are rescaled in few tiles.  RING fragments are read ahead of
@@ -628,11 +651,11 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void packed_wide_fwd_kernel
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        f32x4 v;
+      for (int b = 0; b < 4; b += 2) {
+        f32x4 v[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc[d][4 * b + r] * inv;
-        store4(o + (size_t)q * h + head * DH + 32 * d + 8 * b + 4 * half, v);
+        for (int r = 0; r < 8; ++r) v[r >> 2][r & 3] = acc[d][4 * b + r] * inv;
+        store_pair(o + (size_t)q * h + head * DH + 32 * d + 8 * b, v[0], v[1], half);
       }
   }
   if (q <= last && half == 0) lse[(size_t)head * rows + q] = fmaf(ref, 0.6931471805599453f, __logf(l));
@@ -749,11 +772,11 @@ __device__ __forceinline__ void packed_dq_block(char* smem, int q0, int key_firs
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        f32x4 v;
+      for (int b = 0; b < 4; b += 2) {
+        f32x4 v[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = dq[d][4 * b + r] * scale;
-        store4(dqkv + (size_t)q * ld + head * DH + 32 * d + 8 * b + 4 * half, v);
+        for (int r = 0; r < 8; ++r) v[r >> 2][r & 3] = dq[d][4 * b + r] * scale;
+        store_pair(dqkv + (size_t)q * ld + head * DH + 32 * d + 8 * b, v[0], v[1], half);
       }
   }
   if (redo) redo_packed_dq_rows<bf16, DH>(redo, qw0, plan, qkv, d_o, lse, from_delta, dqkv, h, hkv, group, head, scale, -1.f);
@@ -925,19 +948,19 @@ __device__ __forceinline__ void packed_dkv_block(char* smem, int k0, int query_e
   const uint32_t bad_k = rows_to_redo(not_finite<DT>(dk), total - kw0), bad_v = rows_to_redo(not_finite<DT>(dv), total - kw0);
   const uint32_t redo = keys_to_redo(bad_k, bad_v, lse + stat_at, from_delta + stat_at, min(key, last), group, plan.rows);
   if (key <= last && !(redo >> (lane & 31) & 1)) {
-    bf16* to = out + (size_t)key * ld + 4 * half;
+    bf16* to = out + (size_t)key * ld;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        f32x4 vk, vv;
+      for (int b = 0; b < 4; b += 2) {
+        f32x4 vk[2], vv[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          vk[r] = dk[d][4 * b + r] * scale;
-          vv[r] = dv[d][4 * b + r];
+        for (int r = 0; r < 8; ++r) {
+          vk[r >> 2][r & 3] = dk[d][4 * b + r] * scale;
+          vv[r >> 2][r & 3] = dv[d][4 * b + r];
         }
-        store4(to + 32 * d + 8 * b, vk);
-        store4(to + hkv + 32 * d + 8 * b, vv);
+        store_pair(to + 32 * d + 8 * b, vk[0], vk[1], half);
+        store_pair(to + hkv + 32 * d + 8 * b, vv[0], vv[1], half);
       }
   }
   if (redo)
