@@ -13,11 +13,11 @@
 // waves take a tile each; "wide" with SPLIT = 2, blocks of 64 rows by two pairs of waves that take half of the keys each; "wide" with
 // SPLIT = 1, blocks of 128 rows, 32 a wave, all waves against the same tiles.
 //
-// What bounds them: long sequences the matrix cores' issue (16384 rows in 3 sequences, 40 heads of 128: forward 1001 us, 967 TFLOP/s of
-// the 1135 that a large product reaches on this card; one sequence of 4096 rows, 32 heads of 128: forward 140 us, 980 TFLOP/s, backward
-// 504 us, 545 TFLOP/s, of which two terms of dS are 50 us); short ones what a block does besides its products: its place in the plan, first
-// tiles, masks and results, and the longest sequence's chain of tiles (4096 rows in 21 sequences, 32 heads of 128 over 8: 34 and 98 us; 8192
-// rows in 170, 40 heads of 64 over 8: 32 and 88; 2048 rows in 6, 16 heads of 128: 24 and 50).  Blocks of 32 rows alone took 2870 us for the
+// What bounds them: long sequences the matrix cores' issue (16384 rows in 3 sequences, 40 heads of 128: forward 986 us, 982 TFLOP/s of
+// the 1135 that a large product reaches on this card; one sequence of 4096 rows, 32 heads of 128: forward 139 us, 988 TFLOP/s, backward
+// 497 us, 553 TFLOP/s, of which two terms of dS are 50 us); short ones what a block does besides its products: its place in the plan, first
+// tiles, masks and results, and the longest sequence's chain of tiles (4096 rows in 21 sequences, 32 heads of 128 over 8: 30 and 93 us; 8192
+// rows in 170, 40 heads of 64 over 8: 29 and 78; 2048 rows in 6, 16 heads of 128: 23 and 48).  Blocks of 32 rows alone took 2870 us for the
 // first of these and 88 and 188, 135 and 226, 31 and 84 for the last three.
 //
 // P and dS are rounded to bf16 once on their way into the second product, as the inputs of every product here are (dS for dQ in two
@@ -1124,11 +1124,12 @@ bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void*
     return false;
   if (dtype == kF32)
     return attention_packed_forward_f32((const float*)qkv, plan, (float*)o, lse, rows, h, n_heads, n_kv_heads, stream);
-  // Larger blocks share more of each tile, smaller ones fill more of the 256 CUs and leave shorter chains behind a long sequence.  Forward,
-  // us, few / 64 rows / 128 rows, by heads x blocks of 128 rows; in brackets one sequence, before it 50 to 100:
-  //   heads of 64:   64: 5.9 6.5 7.8 [12.6 23.5 35.7];  128: 9.8 6.7 8.3 [10 sequences 12.8 12.2 18.1];  512: - 11.0 10.2 [- 54 71];
-  //   640: - 16.3 14.2 [- 37 40].   128: 64: 8.0 9.3 10.8;  128: 13.5 9.4 11.8;  256: - 12.6 12.2 [- 36 51];  320: - 18.5 15.5 [2
-  //   sequences - 23.0 24.2];  512: - 23.0 17.4 [- 92 103].
+  // Larger blocks share more of each tile, smaller ones fill more of the 256 CUs and leave shorter chains behind a long sequence; lengths
+  // are not known here.  us, few / 64 rows / 128 rows, sequences of 40 rows, of 800 to 1024, one:
+  //   heads of 64: 64 blocks of 128 rows (all heads) 6.0 6.3 7.8, 10.8 16.5 25.2;  128: 9.3 6.4 7.8, 12.6 13.9 19.6, 25 42 67;
+  //     512: 32 10.7 10.1, 44 23 30, 84 54 70;  640: 42 14.5 12.4, 58 26 30;
+  //   heads of 128: 64: 8.2 8.6 10.0, 14.9 22.4 34.9;  128: 12.9 8.6 10.4, 18.7 18.8 27.2, 40 57 94;  256: 24 11.4 11.3, 36 25 36;
+  //     320: 31 16.1 13.5, 43 23 29;  512: 48 20.7 15.3, 67 33 41, 137 89 102;  640: 60 26 20, 87 45 43.
   const int64_t blocks = (int64_t)n_heads * ceil_div(rows, kPlanBlock);
   auto launch = h / n_heads == 128 ? (blocks <= 64 ? few_forward<128> : blocks <= 384 ? wide_forward<128, 2, 1> : wide_forward<128, 1, 1>)
                                    : (blocks <= 64 ? few_forward<64> : blocks <= 512 ? wide_forward<64, 2, 1> : wide_forward<64, 1, 2>);
@@ -1159,12 +1160,15 @@ bool attention_packed_backward(int dtype, const void* qkv, const int* plan, cons
   if (!(h / n_heads == 128 ? statistics<128> : statistics<64>)((const bf16*)o, (const bf16*)d_o, lse, stats, rows, n_heads, stream))
     return false;
   const int group = n_heads / n_kv_heads, row_blocks = ceil_div(rows, kPlanBlock);
-  // As in the forward; blocks of keys are n_kv_heads x row_blocks and each walks its whole group.  Backward, us:
-  //   few / 64 rows, by n_heads x row_blocks: heads of 128, no groups 32: 12.6 14.4, 64: 18.5 15.1; groups of 4, 128: 26.0 29.9 and, fewer
-  //   and longer sequences, 39.6 63.4; 256: 46.3 32.8 and 61.9 75.5.
-  //   64 rows / 128 rows, by n_kv_heads x row_blocks: heads of 128, 256: 16 heads, 5 sequences 40.8 47.1, one 77 97; 32 heads over 8, 10
-  //   sequences 125 156; 512: 32 over 8, 204 sequences 148 126, 20 sequences 251 226.  Heads of 64, 256: 40 over 8, 10 sequences 87 140;
-  //   16 heads, 5 sequences 23.6 32; 512: 40 over 8, 170 sequences 100 90; 640: 40 heads 42 37; 1024: 32 heads, one sequence 283 275.
+  // As in the forward; blocks of keys are n_kv_heads x row_blocks, and each walks its whole group.  us, as there:
+  //   few or not by n_heads x row_blocks: heads of 64, no groups: 32: 9.7 9.6 11.6, 13.7 20.2 32.3;  64: 14.4 10.0 13.2, 21.2 23.3 37.2;
+  //     groups of 4: 128: 16.8 19.0 28.0, 27 60 108;  256: 31 22 36, 49 73 129 (200 rows each 36 36 56);
+  //     heads of 128, no groups: 32: 12.6 13.0 15.2, 22.8 29.3 44.0;  64: 19.5 13.9 18.0, 33.9 34.2 51.3;
+  //     groups of 4: 128: 26 28 38, 58 90 151;  256: 46 31 50, 85 111 181 (200 rows each 55 53 78);
+  //   64 or 128 rows by n_kv_heads x row_blocks: heads of 64: 256: 42 18.4 16.6, 59 35 50;  groups of 4 106 41 44, 165 107 178, 378 299 463;
+  //     512: 85 30 27, 113 52 61, 216 155 171;  640: 104 35 32, 146 69 67;
+  //     heads of 128: 256: 63 30 26, 101 55 70;  groups of 4 157 74 66, 292 163 250, 782 521 696;  320: 75 37 33, 119 65 61;
+  //     512: 121 56 47, 189 97 89, 429 269 264.
   const bool few = (int64_t)n_heads * row_blocks <= std::min(32 * group, 128), narrow = (int64_t)n_kv_heads * row_blocks <= 256;
   auto launch = h / n_heads == 64 ? (few ? few_backward<64> : narrow ? wide_backward<64, 2, 2> : wide_backward<64, 1, 2>)
                                   : (few ? few_backward<128> : narrow ? wide_backward<128, 2, 2> : wide_backward<128, 1, 3>);
