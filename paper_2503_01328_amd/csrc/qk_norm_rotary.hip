@@ -8,10 +8,10 @@
 // Everything between the load and the one rounding of the store is fp32; angles are formed in fp64 and reduced to a turn there: in
 // fp32 position 10^6 would be a twentieth of a radian off.
 //
-// Bound by memory: each element is read (backward with gains: with its input) and written once.  A wave takes a row at a time: lane p
-// forms the cosine and sine of pair p once for all heads, which read them back from LDS; then 64 / LANES heads at a time, a lane holding 16
-// elements (eight pairs) of one head.  bf16, 16384 rows, 40 heads of 128 over 8: forward 94 us, 5.0 TB/s, backward 140 us, 4.8 TB/s (a
-// large copy reaches 4.9); 2048 rows, 16 heads: 11.1 us, 4.5 TB/s, and 17.9 us.
+// Bound by memory: each element is read (backward with gains: with its input) and written once.  A wave takes a row at a time, or shares
+// one with others (waves_of_a_row): lane p forms the cosine and sine of pair p once for all heads, which read them back from LDS; then
+// 64 / LANES heads at a time, a lane holding 16 elements (eight pairs) of one head.  bf16, from HBM: 16384 rows, 40 heads of 128 over 8:
+// forward 91 us, backward 145 us (a large copy reaches 4.9 TB/s); 2048 rows, 16 heads: 13.6 us, and 24.0 us.
 // The gains' gradients stay in registers over all rows of a wave, are added over the lanes and waves of a block in a fixed order, and a
 // second launch adds the blocks: no atomics.  Half of those blocks take the queries and half the keys and values, so that a lane has one
 // gain's gradient to hold, not two, and twice the waves fit: 189 us without, 140 with.
@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kBlocks = 1024;  // for queries and for keys at most in the backward; each leaves a partial sum of a gain's gradient
 constexpr int kMaxPairs = 128;
-constexpr int kMaxRows = 1 << 25;  // a block of 256 threads for four of them: 2^31 threads
+constexpr int kMaxRows = 1 << 25, kMaxBlocks = 1 << 23;  // 2^31 threads
 
 struct Axes {
   int end[kMaxRotaryAxes];  // the pairs [end[i - 1], end[i]) turn by axis i
@@ -108,7 +108,7 @@ template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD>
 __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const T* __restrict__ x_in, const T* __restrict__ gain_q,
                                                              const T* __restrict__ gain_k, const int* __restrict__ positions,
                                                              const float* __restrict__ inv_freq, Axes axes, T* out,
-                                                             float* __restrict__ partials, Shape s) {
+                                                             float* __restrict__ partials, Shape s, int split) {
   __shared__ float2 turns[4][kMaxPairs];
   __shared__ __align__(16) float gains[2 * LANES][16];  // for queries, for keys
   __shared__ float sums[BACKWARD ? 4 : 1][BACKWARD ? 16 * LANES : 1];
@@ -137,7 +137,8 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
   const int blocks = parts ? gridDim.x / 2 : gridDim.x, part = (int)blockIdx.x >= blocks, block = blockIdx.x - part * blocks;
   const int head_first = part ? s.n_heads : 0, head_end = parts && !part ? s.n_heads : s.n_heads + s.n_kv_heads;
 
-  for (int row = block * 4 + wave; row < s.rows; row += blocks * 4) {
+  const int share = wave & (split - 1), shared = 4 / split;  // `split` waves share a row, `shared` rows a block
+  for (int row = block * shared + wave / split; row < s.rows; row += blocks * shared) {
     if (positions[row] < 0) continue;  // no token there
     for (int p = lane; p < s.pairs; p += 64) {
       int axis = 0;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
       sn[i] = BACKWARD ? -cs.y : cs.y;
     }
     wave_sync();
-    for (int head0 = head_first; head0 < head_end; head0 += HEADS) {
+    for (int head0 = head_first + share * HEADS; head0 < head_end; head0 += split * HEADS) {
       const int head = head0 + lane / LANES;
       const bool mine = held && head < head_end;
       const size_t at = (size_t)row * ld + (size_t)head * s.dh;
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
     if (in != out && (!parts || part)) {  // the values pass
       constexpr int V = Vec16<T>::N;
       const size_t v0 = (size_t)row * ld + s.h + s.hkv;
-      for (int e = lane * V; e < s.hkv; e += 64 * V) store16(out + v0 + e, load16(in + v0 + e));
+      for (int e = (share * 64 + lane) * V; e < s.hkv; e += split * 64 * V) store16(out + v0 + e, load16(in + v0 + e));
     }
   }
   if constexpr (BACKWARD) {
@@ -305,35 +306,52 @@ bool check(const char* what, const QkNormRotary& a, const void* in, const void* 
   return true;
 }
 
+int lanes_of_a_head(int dh) { return dh <= 32 ? 2 : dh <= 64 ? 4 : dh <= 128 ? 8 : 16; }
+
 template <typename T, int LANES, bool BACKWARD>
 void launch(const QkNormRotary& a, const void* in, const void* x_in, void* out, float* partials, const Axes& axes, const Shape& s,
-            int blocks, hipStream_t stream) {
+            int blocks, int split, hipStream_t stream) {
   auto k = a.layout == kRotaryNeighbours ? qk_norm_rotary_kernel<T, LANES, true, BACKWARD> : qk_norm_rotary_kernel<T, LANES, false, BACKWARD>;
   k<<<blocks, 256, 0, stream>>>((const T*)in, (const T*)x_in, (const T*)a.gain_q, (const T*)a.gain_k, a.positions, a.inv_freq, axes,
-                                (T*)out, partials, s);
+                                (T*)out, partials, s, split);
 }
 template <bool BACKWARD>
 void launch(int dtype, const QkNormRotary& a, const void* in, const void* x_in, void* out, float* partials, const Axes& axes,
-            const Shape& s, int blocks, hipStream_t stream) {
-  auto k = s.dh <= 32    ? (dtype == kF32 ? launch<float, 2, BACKWARD> : launch<bf16, 2, BACKWARD>)
-           : s.dh <= 64  ? (dtype == kF32 ? launch<float, 4, BACKWARD> : launch<bf16, 4, BACKWARD>)
-           : s.dh <= 128 ? (dtype == kF32 ? launch<float, 8, BACKWARD> : launch<bf16, 8, BACKWARD>)
-                         : (dtype == kF32 ? launch<float, 16, BACKWARD> : launch<bf16, 16, BACKWARD>);
-  k(a, in, x_in, out, partials, axes, s, blocks, stream);
+            const Shape& s, int blocks, int split, hipStream_t stream) {
+  const int lanes = lanes_of_a_head(s.dh);
+  auto k = lanes == 2   ? (dtype == kF32 ? launch<float, 2, BACKWARD> : launch<bf16, 2, BACKWARD>)
+           : lanes == 4 ? (dtype == kF32 ? launch<float, 4, BACKWARD> : launch<bf16, 4, BACKWARD>)
+           : lanes == 8 ? (dtype == kF32 ? launch<float, 8, BACKWARD> : launch<bf16, 8, BACKWARD>)
+                        : (dtype == kF32 ? launch<float, 16, BACKWARD> : launch<bf16, 16, BACKWARD>);
+  k(a, in, x_in, out, partials, axes, s, blocks, split, stream);
 }
-int backward_blocks(int rows) { return std::min(ceil_div(rows, 4), kBlocks); }
+// How many waves share a row of `heads` heads.  Few rows: the wave's chain of loads, heads after heads, is what such a launch waits for.
+// Many: two waves to a row still leave less of the card idle towards the end where a row has three steps of heads, angles formed twice cost
+// more than that where it has fewer.  With gains' gradients a launch has two kinds of blocks and its partial sums grow with the blocks.
+// bf16 from HBM, us, one wave / two / four: 40 heads of 128 over 8, forward 128 rows 8.9 6.1 5.4, 1000 rows 14.0 10.5 10.5, 2048 rows 16.7
+// 15.6 17.2, 16384 rows 97 91 91; 16 heads of 64 over 4 (two steps) 5.3 4.5 4.6 (500 rows), 9.9 11.8 14.6 (4096).  Backward with gains: 128
+// rows 14.5 11.4 10.3, 500 rows 18.3 15.1 14.5, 1000 rows 20.0 18.5 23.9, 2048 rows 25.9 30.5 35.0; 16 heads of 64 (one step), 500
+// rows 9.4 9.5 11.7.
+int waves_of_a_row(int rows, int dh, int heads, bool gains) {
+  const int steps = ceil_div(heads, 64 / lanes_of_a_head(dh)), most = steps > 2 ? 4 : steps;
+  if (gains) return rows <= 512 ? most : rows <= 1024 ? std::min(most, 2) : 1;
+  return rows <= 1024 ? most : steps > 2 ? 2 : 1;
+}
+int blocks_of(int rows, int split, int most) { return (int)std::min<int64_t>(ceil_div64((int64_t)rows * split, 4), most); }
 
 }  // namespace
 
 size_t qk_norm_rotary_backward_workspace(int rows, int h, int n_heads) {
-  return (size_t)backward_blocks(rows) * 2 * (h / n_heads) * sizeof(float);
+  const int dh = h / n_heads;
+  return (size_t)blocks_of(rows, waves_of_a_row(rows, dh, n_heads, true), kBlocks) * 2 * dh * sizeof(float);
 }
 
 bool qk_norm_rotary_forward(int dtype, const QkNormRotary& a, const void* qkv, void* out, hipStream_t stream) {
   Axes axes;
   Shape s;
   if (!check("qk_norm_rotary_forward", a, qkv, nullptr, out, axes, s)) return false;
-  launch<false>(dtype, a, qkv, nullptr, out, nullptr, axes, s, ceil_div(a.rows, 4), stream);
+  const int split = waves_of_a_row(a.rows, s.dh, a.n_heads + a.n_kv_heads, false);
+  launch<false>(dtype, a, qkv, nullptr, out, nullptr, axes, s, blocks_of(a.rows, split, kMaxBlocks), split, stream);
   return launch_ok("qk_norm_rotary_kernel");
 }
 
@@ -351,8 +369,9 @@ bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out
     set_error("qk_norm_rotary_backward: dqkv may be d_out, but not qkv");
     return false;
   }
-  const int blocks = backward_blocks(a.rows);
-  launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, a.gain_q ? 2 * blocks : ceil_div(a.rows, 4), stream);
+  const int split = waves_of_a_row(a.rows, s.dh, a.gain_q ? a.n_heads : a.n_heads + a.n_kv_heads, a.gain_q != nullptr);
+  const int blocks = blocks_of(a.rows, split, a.gain_q ? kBlocks : kMaxBlocks);
+  launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, a.gain_q ? 2 * blocks : blocks, split, stream);
   if (a.gain_q) rotary_gain_sum_kernel<<<2 * s.dh / 8, 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
   return launch_ok("qk_norm_rotary_kernel");
 }

@@ -376,6 +376,14 @@ def test_norm_and_rotation(gpu_device, dtype, in_place, dh, a, akv, rows, axis_p
     _rotary_case(gpu_device, dtype, dh, a, akv, rows, axis_pairs, neighbours, norm, 2 ** 20, in_place)
 
 
+# one, two or four waves to a row, by rows and heads, with shares of them that have no heads
+@pytest.mark.parametrize("rows", [511, 513, 1023, 1025, 4101])
+@pytest.mark.parametrize("dtype,dh,a,akv,norm", [("bf16", 128, 40, 8, True), ("f32", 128, 9, 9, True), ("bf16", 64, 24, 8, False), ("bf16", 256, 10, 1, True),
+                                                 ("f32", 32, 33, 1, True)])
+def test_norm_and_rotation_of_shared_rows(gpu_device, dtype, dh, a, akv, norm, rows):
+    _rotary_case(gpu_device, dtype, dh, a, akv, rows, [8, dh // 4], False, norm, 2 ** 20, True)
+
+
 @pytest.mark.parametrize("far", [0, 1, 2 ** 31 - 1])
 def test_rotation_of_the_first_and_the_last_positions(gpu_device, far):
     _rotary_case(gpu_device, "f32", 128, 2, 1, 40, [40, 24], False, True, far, False)
