@@ -319,8 +319,8 @@ int po_op_attention_backward(int32_t dtype, const void* qkv, const void* o, cons
  *
  * The maps of such a batch, built on the GPU from its lengths (DEVICE int32 [n_sequences]), all int32 in DEVICE memory, any of them
  * NULL if not wanted: starts [n_sequences + 1] (the first row of each and the row behind the last), positions [rows] (of a
- * row in its sequence), sequence [rows] (whose row it is), the last two -1 behind the last sequence; and plan, po_op_packed_plan_bytes(rows) bytes, 16-byte
- * aligned, which the attention calls below read: one plan serves every layer.  A length below zero counts as zero; sequences
+ * row in its sequence), sequence [rows] (whose row it is), the last two -1 behind the last sequence; and plan, po_op_packed_plan_bytes(rows)
+ * bytes, 16-byte aligned, which the attention calls below read: one plan serves every layer.  A length below zero counts as zero; sequences
  * that reach past `rows` are cut there.  1 to 16384 sequences, 1 to 2097152 rows (beyond: PO_E_INVAL, and 0 bytes). */
 uint64_t po_op_packed_plan_bytes(int32_t rows);
 int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows, int32_t* starts, int32_t* positions,
@@ -330,8 +330,9 @@ int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows,
  * d_o [rows, h], lse [n_heads, rows], dqkv like qkv, head sizes 64 and 128, all tensors 16-byte aligned.  plan: as po_op_packed_plan left it
  * for the same `rows` (of one made for another row count nothing is computed).  Rows behind the last sequence are not read as
  * keys or queries and left as they were in every output.  An infinity or NaN in a row of one sequence reaches no other sequence,
- * in a key or value row no row of o and dQ before it.  dqkv is neither qkv nor d_o.  workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned,
- * contents unspecified before and afterwards.  Results do not depend on how often or beside what a call runs: no atomics. */
+ * in a key or value row no row of o and dQ before it.  dqkv is neither qkv nor d_o.
+ * workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned, contents unspecified before and afterwards.
+ * Results do not depend on how often or beside what a call runs: no atomics. */
 int po_op_attention_packed_forward(int32_t dtype, const void* qkv, const void* plan, void* o, float* lse, int32_t rows, int32_t h,
                                    int32_t n_heads, int32_t n_kv_heads, void* stream);
 uint64_t po_op_attention_packed_backward_workspace(int32_t dtype, int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads);
@@ -352,8 +353,8 @@ int po_op_qk_norm_rotary_forward(int32_t dtype, const void* qkv, const void* gai
                                  const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes, int32_t layout, void* out,
                                  int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream);
 /* dqkv [rows, h + 2 hkv] = the gradient of qkv from that of out, d_out (dqkv may be d_out itself, not qkv); dgain_q, dgain_k [head
- * size] fp32: += the gains' gradients, in a fixed order.  qkv is the input of the forward.  Without gains qkv, dgain_q, dgain_k and
- * workspace may be NULL.  workspace: po_op_qk_norm_rotary_backward_workspace bytes, contents unspecified afterwards. */
+ * size] fp32: += the gains' gradients, in a fixed order; one and the same tensor for a gain that both share.  qkv is the input of the
+ * forward.  Without gains qkv, dgain_q, dgain_k and workspace may be NULL.  workspace: po_op_qk_norm_rotary_backward_workspace bytes, contents unspecified afterwards. */
 uint64_t po_op_qk_norm_rotary_backward_workspace(int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads);
 int po_op_qk_norm_rotary_backward(int32_t dtype, const void* d_out, const void* qkv, const void* gain_q, const void* gain_k,
                                   const int32_t* positions, const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes,

@@ -372,7 +372,10 @@ bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out
   const int split = waves_of_a_row(a.rows, s.dh, a.gain_q ? a.n_heads : a.n_heads + a.n_kv_heads, a.gain_q != nullptr);
   const int blocks = blocks_of(a.rows, split, a.gain_q ? kBlocks : kMaxBlocks);
   launch<true>(dtype, a, d_out, qkv, dqkv, workspace, axes, s, a.gain_q ? 2 * blocks : blocks, split, stream);
-  if (a.gain_q) rotary_gain_sum_kernel<<<2 * s.dh / 8, 256, 0, stream>>>(workspace, blocks, s.dh, dgain_q, dgain_k);
+  // one gain for both: the partial sums of queries and of keys are one array of twice the blocks, and its columns added to once
+  const bool shared = dgain_q == dgain_k;
+  if (a.gain_q)
+    rotary_gain_sum_kernel<<<(shared ? 1 : 2) * s.dh / 8, 256, 0, stream>>>(workspace, shared ? 2 * blocks : blocks, s.dh, dgain_q, dgain_k);
   return launch_ok("qk_norm_rotary_kernel");
 }
 

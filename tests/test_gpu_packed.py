@@ -414,6 +414,21 @@ def test_norm_and_rotation_gradient_is_that_of_differences(gpu_device, dtype):
         assert abs(float((got.double() * d).sum()) - slope) <= float((t * d.abs()).sum()) + 1e-6 * (abs(slope) + 1)
 
 
+def test_a_gain_that_queries_and_keys_share(gpu_device):
+    dh, a, akv, rows = 128, 8, 4, 300
+    h, hkv, g = a * dh, akv * dh, _gen(gpu_device, 7)
+    qkv, d_out = (torch.randn(rows, h + 2 * hkv, generator=g, device=gpu_device).bfloat16() for _ in range(2))
+    gain, start = torch.rand(dh, generator=g, device=gpu_device).bfloat16(), torch.randn(dh, generator=g, device=gpu_device)
+    positions = torch.arange(rows, device=gpu_device, dtype=torch.int32)
+    inv_freq = torch.rand(64, generator=g, device=gpu_device)
+    ws = torch.empty(po.po_op_qk_norm_rotary_backward_workspace(rows, h, a, akv), dtype=torch.uint8, device=gpu_device)
+    dqkv, of_both = torch.empty_like(qkv), start.clone()
+    po.po_op_qk_norm_rotary_backward(po.PO_BF16, d_out, qkv, gain, gain, positions, inv_freq, [64], 0, dqkv, of_both, of_both, ws, rows, h, a, akv)
+    want, tol = ref.rotary(qkv, gain, gain, positions[None], inv_freq, [64], False, h, a, akv, 1e-6, d_out)
+    both = want["dgain_q"] + want["dgain_k"]  # one sum of both, and the addition to what was there
+    _within(of_both, start.double() + both, tol["dgain_q"] + tol["dgain_k"] + 2 * ref.E * (start.double().abs() + 2 * both.abs()), "dgain")
+
+
 def test_rotation_keeps_what_is_not_rotated(gpu_device):
     """Elements behind the pairs pass bit for bit, infinities among them."""
     dh, rows = 128, 5
