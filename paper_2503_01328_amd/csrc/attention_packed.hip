@@ -1122,6 +1122,10 @@ bool attention_packed_forward(int dtype, const void* qkv, const int* plan, void*
   if (!check("attention_packed_forward", dtype, rows, h, n_heads, n_kv_heads, plan, (uintptr_t)qkv | (uintptr_t)o,
              !qkv || !plan || !o || !lse, (uintptr_t)lse))
     return false;
+  if (o == qkv) {
+    set_error("attention_packed_forward: o is another tensor than qkv");
+    return false;
+  }
   if (dtype == kF32)
     return attention_packed_forward_f32((const float*)qkv, plan, (float*)o, lse, rows, h, n_heads, n_kv_heads, stream);
   // Larger blocks share more of each tile, smaller ones fill more of the 256 CUs and leave shorter chains behind a long sequence; lengths

@@ -69,6 +69,12 @@ def test_attention_backward_refuses_its_inputs_as_output(dtype, other):
     _refused(f, "another tensor", *args, stream=0)
 
 
+@pytest.mark.parametrize("dtype", [po.PO_F32, po.PO_BF16])
+def test_attention_forward_refuses_its_input_as_output(dtype):
+    f, args = _forward(dtype, GOOD)
+    _refused(f, "another tensor", *args, stream=0)
+
+
 @pytest.mark.parametrize("call", [_forward, _backward])
 def test_attention_refuses_types(call):
     f, args = call(2, GOOD)
