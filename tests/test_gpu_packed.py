@@ -46,7 +46,8 @@ def _random_lengths(seed, n, most):
 
 LENGTHS = [([1], 1), ([5], 9), ([0, 3, 0, 1, 0], 4), ([0], 3), ([-4, 6, -1, 2], 20), ([10, 2000, 5], 700), ([2 ** 31 - 1] * 3, 200),
            ([128, 128], 256), ([127, 1, 129, 64], 400), (_random_lengths(1, 1500, 9), 4500), (_random_lengths(2, 16384, 40), 200000),
-           (_random_lengths(3, 1024, 5), 1024), (_random_lengths(4, 1025, 5), 2000), ([1] * 5000, 5000), ([2097152], 2097152)]
+           (_random_lengths(3, 1024, 5), 1024), (_random_lengths(4, 1025, 5), 2000), ([1] * 5000, 5000), ([2097152], 2097152),
+           (_random_lengths(5, 16384, 100), 900001)]
 
 
 @pytest.mark.parametrize("lengths,rows", LENGTHS, ids=lambda v: str(len(v)) if isinstance(v, list) else str(v))
