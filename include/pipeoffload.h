@@ -331,7 +331,8 @@ int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows,
  * for the same `rows` (of one made for another row count nothing is computed).  Rows behind the last sequence are not read as
  * keys or queries and left as they were in every output.  An infinity or NaN in a row of one sequence reaches no other sequence,
  * in a key or value row no row of o and dQ before it.  o is not qkv, dqkv neither qkv nor d_o.
- * workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned, contents unspecified before and afterwards.
+ * workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned, contents unspecified before and afterwards; one for more
+ * rows (of the same type and heads) serves fewer.
  * Results do not depend on how often or beside what a call runs: no atomics. */
 int po_op_attention_packed_forward(int32_t dtype, const void* qkv, const void* plan, void* o, float* lse, int32_t rows, int32_t h,
                                    int32_t n_heads, int32_t n_kv_heads, void* stream);

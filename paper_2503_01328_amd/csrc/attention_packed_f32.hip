@@ -6,6 +6,8 @@
 // 4 sequences, forward 22 us, backward 54 with its sums, against 13 us of products at the rate of a large one.
 // Eight waves for heads of 64, which LDS has room for, gain where chains of tiles are long for the launch (this shape's backward with
 // whole groups 61.1 -> 55.9 us) and lose elsewhere (16 heads, 4000 rows of 60 sequences 111 -> 158, 32 heads, 3000 rows 1090 -> 1176).
+#include <algorithm>
+
 #include "attention_f32_tile.h"
 #include "attention_packed_rows.h"
 
@@ -311,11 +313,13 @@ __global__ __launch_bounds__(256) void packed_f32_sum_kernel(const float* __rest
 // Heads that share keys: a dK/dV block a query head, added up afterwards, while the blocks of whole groups, whose chains are that much
 // longer, would fill half of the CUs at most.  Backward, us, whole groups / by heads: 12 heads of 64 over 4, 1000 rows of 4 sequences (128
 // blocks) 61 / 45; 16 heads of 128 over 4, 2000 rows (252) 263 / 272; 32 heads of 128 over 8, 2048 rows (512) 1184 / 1249.
-static bool by_heads(int rows, int n_heads, int n_kv_heads) {
-  return n_heads > n_kv_heads && (int64_t)n_kv_heads * ceil_div(rows, 32) <= 128;
+static int rows_by_heads(int n_heads, int n_kv_heads) {  // up to how many rows
+  return n_heads > n_kv_heads ? 128 / n_kv_heads * 32 : 0;
 }
+static bool by_heads(int rows, int n_heads, int n_kv_heads) { return rows <= rows_by_heads(n_heads, n_kv_heads); }
+// What any count of rows up to `rows` needs: a workspace for a program's largest batch serves its smaller ones.
 size_t attention_packed_f32_partials(int rows, int h, int n_heads, int n_kv_heads) {
-  return by_heads(rows, n_heads, n_kv_heads) ? (size_t)rows * 2 * h : 0;  // group * 2 hkv columns
+  return (size_t)std::min(rows, rows_by_heads(n_heads, n_kv_heads)) * 2 * h;  // group * 2 hkv columns
 }
 
 template <int DH>

@@ -91,6 +91,15 @@ def test_workspaces():
         assert po.po_op_qk_norm_rotary_backward_workspace(*bad) == 0
 
 
+@pytest.mark.parametrize("dtype", [po.PO_F32, po.PO_BF16])
+@pytest.mark.parametrize("dh,a,akv", [(64, 12, 4), (128, 40, 8), (64, 8, 1), (64, 3, 3), (128, 256, 128), (64, 400, 200)])
+def test_attention_workspace_for_more_rows_serves_fewer(dtype, dh, a, akv):
+    """A program keeps one workspace, of the size that its largest batch asks for."""
+    sizes = [po.po_op_attention_packed_backward_workspace(dtype, rows, a * dh, a, akv) for rows in range(1, 5000)]
+    assert all(x <= y for x, y in zip(sizes, sizes[1:]))
+    assert po.po_op_attention_packed_backward_workspace(dtype, 2097152, a * dh, a, akv) >= sizes[-1]
+
+
 ROT = dict(qkv=AT, gain_q=AT, gain_k=AT, positions=AT, inv_freq=AT, axis_pairs=[32], layout=0, out=AT, d_out=AT, dqkv=AT + 64, dgain_q=AT, dgain_k=AT,
            workspace=AT, rows=10, h=256, n_heads=4, n_kv_heads=2, eps=1e-6)
 BAD_ROT = [dict(rows=0), dict(rows=2 ** 25 + 1), dict(h=0), dict(n_heads=0), dict(n_heads=3), dict(n_kv_heads=3), dict(h=4 * 24), dict(h=4 * 8), dict(h=4 * 272),
