@@ -355,7 +355,8 @@ int po_op_qk_norm_rotary_forward(int32_t dtype, const void* qkv, const void* gai
                                  int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads, float eps, void* stream);
 /* dqkv [rows, h + 2 hkv] = the gradient of qkv from that of out, d_out (dqkv may be d_out itself, not qkv); dgain_q, dgain_k [head
  * size] fp32: += the gains' gradients, in a fixed order; one and the same tensor for a gain that both share.  qkv is the input of the
- * forward.  Without gains qkv, dgain_q, dgain_k and workspace may be NULL.  workspace: po_op_qk_norm_rotary_backward_workspace bytes, contents unspecified afterwards. */
+ * forward.  Without gains qkv, dgain_q, dgain_k and workspace may be NULL.  workspace: po_op_qk_norm_rotary_backward_workspace bytes,
+ * contents unspecified afterwards; one for more rows (of the same heads) serves fewer. */
 uint64_t po_op_qk_norm_rotary_backward_workspace(int32_t rows, int32_t h, int32_t n_heads, int32_t n_kv_heads);
 int po_op_qk_norm_rotary_backward(int32_t dtype, const void* d_out, const void* qkv, const void* gain_q, const void* gain_k,
                                   const int32_t* positions, const float* inv_freq, const int32_t* axis_pairs, int32_t n_axes,

@@ -337,13 +337,15 @@ int waves_of_a_row(int rows, int dh, int heads, bool gains) {
   if (gains) return rows <= 512 ? most : rows <= 1024 ? std::min(most, 2) : 1;
   return rows <= 1024 ? most : steps > 2 ? 2 : 1;
 }
+// (split is at most 4: no more blocks than rows)
 int blocks_of(int rows, int split, int most) { return (int)std::min<int64_t>(ceil_div64((int64_t)rows * split, 4), most); }
 
 }  // namespace
 
+// What any count of rows up to `rows` needs, for a program that keeps one workspace for its largest batch: fewer rows can make more
+// blocks, as more waves share each, but never more than rows.
 size_t qk_norm_rotary_backward_workspace(int rows, int h, int n_heads) {
-  const int dh = h / n_heads;
-  return (size_t)blocks_of(rows, waves_of_a_row(rows, dh, n_heads, true), kBlocks) * 2 * dh * sizeof(float);
+  return (size_t)std::min(rows, kBlocks) * 2 * (h / n_heads) * sizeof(float);
 }
 
 bool qk_norm_rotary_forward(int dtype, const QkNormRotary& a, const void* qkv, void* out, hipStream_t stream) {

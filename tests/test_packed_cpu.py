@@ -119,6 +119,13 @@ def _rot_backward(dtype, c):
                                                                       "dqkv", "dgain_q", "dgain_k", "workspace", "rows", "h", "n_heads", "n_kv_heads", "eps")]
 
 
+@pytest.mark.parametrize("dh,a,akv", [(128, 40, 8), (64, 8, 2), (64, 40, 8), (128, 16, 16), (32, 33, 1), (256, 10, 1), (16, 1, 1)])
+def test_rotary_workspace_for_more_rows_serves_fewer(dh, a, akv):
+    sizes = [po.po_op_qk_norm_rotary_backward_workspace(rows, a * dh, a, akv) for rows in range(1, 9000)]
+    assert all(x <= y for x, y in zip(sizes, sizes[1:]))
+    assert po.po_op_qk_norm_rotary_backward_workspace(2 ** 25, a * dh, a, akv) >= sizes[-1]
+
+
 @pytest.mark.parametrize("dtype", [po.PO_F32, po.PO_BF16])
 @pytest.mark.parametrize("call,more", [(_rot_forward, [dict(qkv=None), dict(out=None), dict(qkv=AT + 8), dict(out=AT + 4)]),
                                        (_rot_backward, [dict(d_out=None), dict(dqkv=None), dict(qkv=None), dict(dgain_q=None), dict(dgain_k=None),
