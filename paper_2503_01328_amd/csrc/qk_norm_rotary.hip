@@ -4,7 +4,7 @@
 //   r = 1 / sqrt(mean(x^2) + eps), y = x r g (one gain for all query heads, one for all key heads; no norm: y = x)
 //   pair p = elements (a, b) of y, angle t = position[axis of p] inv_freq[p]:  (a cos t - b sin t, a sin t + b cos t)
 // backward, d the gradient of the output: u = the rotation by -t of d,
-//   dg += sum over rows and heads of u x r,  w = u g,  dx = r w - x (r^3 / head size) sum(w x)
+//   dg += sum over rows and heads of u x r,  w = u g,  dx = r (w - x r mean(w x r))
 // Everything between the load and the one rounding of the store is fp32; angles are formed in fp64 and reduced to a turn there: in
 // fp32 position 10^6 would be a twentieth of a radian off.
 //
@@ -187,24 +187,27 @@ __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(const T* in, const 
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
           if (mine) load_pairs<T, NEIGHBOURS>(x, y, x_in + at, at_a, at_b);
-          float w[8], z[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+          // The normed x from here on: its products stay in range wherever its own squares did, r^3 does not
+          const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            w[i] = a[i] * gain[i];
-            z[i] = b[i] * gain[8 + i];
-            sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-            dot = fmaf(w[i], x[i], fmaf(z[i], y[i], dot));
-          }
-          const float r = rsqrtf(sum_over_head<LANES>(sq) / (float)s.dh + s.eps);
-          const float f = r * r * r * (sum_over_head<LANES>(dot) / (float)s.dh);
-          if (mine) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              dg_a[i] = fmaf(a[i] * x[i], r, dg_a[i]);
-              dg_b[i] = fmaf(b[i] * y[i], r, dg_b[i]);
-              a[i] = r * w[i] - x[i] * f;
-              b[i] = r * z[i] - y[i] * f;
+            x[i] *= r;
+            y[i] *= r;
+            if (mine) {
+              dg_a[i] = fmaf(a[i], x[i], dg_a[i]);
+              dg_b[i] = fmaf(b[i], y[i], dg_b[i]);
             }
+            a[i] *= gain[i];
+            b[i] *= gain[8 + i];
+            dot = fmaf(a[i], x[i], fmaf(b[i], y[i], dot));
+          }
+          const float mean = sum_over_head<LANES>(dot) / (float)s.dh;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            a[i] = r * (a[i] - x[i] * mean);
+            b[i] = r * (b[i] - y[i] * mean);
           }
         }
       }

@@ -415,6 +415,29 @@ def test_norm_and_rotation_gradient_is_that_of_differences(gpu_device, dtype):
         assert abs(float((got.double() * d).sum()) - slope) <= float((t * d.abs()).sum()) + 1e-6 * (abs(slope) + 1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("size,eps", [(1e15, 1e-6), (1e-15, 0.0), (0.0, 1e-30)])
+def test_norm_gradient_where_r_cubed_is_out_of_range(gpu_device, dtype, dh, size, eps):
+    """Heads so large or small that r^3 is no fp32 number, while x, r and the gradient are: within the bounds of any other head."""
+    code, tdt = DT[dtype]
+    a, akv, rows, g = 4, 2, 37, _gen(gpu_device, 4)
+    h, hkv = a * dh, akv * dh
+    rand = lambda *s: torch.randn(*s, generator=g, device=gpu_device)
+    qkv, d_out = (size * rand(rows, h + 2 * hkv)).to(tdt), rand(rows, h + 2 * hkv).to(tdt)
+    gq, gk = (1 + 0.2 * rand(dh)).to(tdt), (1 + 0.2 * rand(dh)).to(tdt)
+    positions = torch.arange(rows, device=gpu_device, dtype=torch.int32)
+    inv_freq = (10000.0 ** (-torch.arange(dh // 2, device=gpu_device) / (dh // 2))).float()
+    rot = (gq, gk, positions, inv_freq, [dh // 2], 0)
+    out, dqkv, dg = torch.empty_like(qkv), torch.empty_like(qkv), torch.zeros(2, dh, device=gpu_device)
+    ws = torch.empty(po.po_op_qk_norm_rotary_backward_workspace(rows, h, a, akv), dtype=torch.uint8, device=gpu_device)
+    po.po_op_qk_norm_rotary_forward(code, qkv, *rot, out, rows, h, a, akv, eps)
+    po.po_op_qk_norm_rotary_backward(code, d_out, qkv, *rot, dqkv, dg[0], dg[1], ws, rows, h, a, akv, eps)
+    want, tol = ref.rotary(qkv, gq, gk, positions[None], inv_freq, [dh // 2], False, h, a, akv, eps, d_out)
+    for got, k in ((out, "out"), (dqkv, "dqkv"), (dg[0], "dgain_q"), (dg[1], "dgain_k")):
+        _within(got, want[k], tol[k], k)
+
+
 def test_a_gain_that_queries_and_keys_share(gpu_device):
     dh, a, akv, rows = 128, 8, 4, 300
     h, hkv, g = a * dh, akv * dh, _gen(gpu_device, 7)
