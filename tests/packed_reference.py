@@ -16,9 +16,10 @@ def half_step(dtype):
     return torch.finfo(dtype).eps / 2
 
 
-def attention(qkv, d_o, lengths, h, a, akv, o=None):
+def attention(qkv, d_o, lengths, h, a, akv, o=None, absent=None):
     """o, lse, dqkv in 64 bits and their bounds, of qkv [rows, ..] (any float type; bounds for its type) and d_o; rows of no sequence
-    are NaN."""
+    are NaN.  absent [rows]: keys whose scores are -inf whatever qkv says; rows that see no other key must be left out by the caller, with the
+    gradients of the keys that they see."""
     dt, dev, rows, dh = qkv.dtype, qkv.device, qkv.shape[0], h // a
     u, hkv, group, scale = half_step(dt), akv * dh, a // akv, 1 / math.sqrt(dh)
     new = lambda *s: torch.full(s, math.nan, dtype=torch.float64, device=dev)
@@ -35,6 +36,8 @@ def attention(qkv, d_o, lengths, h, a, akv, o=None):
         k, v = (heads(y, akv).repeat_interleave(group, 0) for y in x[:, h:].split(hkv, 1))
         d = heads(d, a)
         hidden = torch.ones(n, n, dtype=torch.bool, device=dev).triu(1)
+        if absent is not None:
+            hidden |= absent[s] & ~(hidden | absent[s]).all(1, keepdim=True)
         sc = (q @ k.mT * scale).masked_fill(hidden, -math.inf)
         lse = torch.logsumexp(sc, -1)
         p = torch.exp(sc - lse[..., None])
