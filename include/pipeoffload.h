@@ -321,7 +321,7 @@ int po_op_attention_backward(int32_t dtype, const void* qkv, const void* o, cons
  * NULL if not wanted: starts [n_sequences + 1] (the first row of each and the row behind the last), positions [rows] (of a
  * row in its sequence), sequence [rows] (whose row it is), the last two -1 behind the last sequence; and plan, po_op_packed_plan_bytes(rows)
  * bytes, 16-byte aligned, which the attention calls below read: one plan serves every layer.  A length below zero counts as zero; sequences
- * that reach past `rows` are cut there.  1 to 16384 sequences, 1 to 2097152 rows (beyond: PO_E_INVAL, and 0 bytes). */
+ * that reach past `rows` are cut there.  None of the arrays overlaps another (PO_E_INVAL).  1 to 16384 sequences, 1 to 2097152 rows (beyond: PO_E_INVAL, and 0 bytes). */
 uint64_t po_op_packed_plan_bytes(int32_t rows);
 int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows, int32_t* starts, int32_t* positions,
                       int32_t* sequence, void* plan, void* stream);

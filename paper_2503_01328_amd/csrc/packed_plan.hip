@@ -139,6 +139,19 @@ bool packed_plan(const int* lengths, int n, int rows, int* starts, int* position
     return false;
   }
   const PackedPlan p{plan, rows};
+  // Blocks read the lengths while others write: a plan from lengths that change meanwhile would name blocks that are none.
+  const struct {
+    uintptr_t at;
+    size_t bytes;
+  } arrays[] = {{(uintptr_t)lengths, 4 * (size_t)n}, {(uintptr_t)starts, 4 * ((size_t)n + 1)}, {(uintptr_t)positions, 4 * (size_t)rows},
+                {(uintptr_t)sequence, 4 * (size_t)rows}, {(uintptr_t)plan, packed_plan_bytes(rows)}};
+  for (const auto& a : arrays)
+    for (const auto& b : arrays)
+      if (a.at % 4 != 0 || (&a != &b && a.at && b.at && a.at < b.at + b.bytes && b.at < a.at + a.bytes)) {
+        set_error("packed_plan: lengths=%p starts=%p positions=%p sequence=%p plan=%p (4-byte aligned, and none overlaps another)",
+                  (const void*)lengths, (void*)starts, (void*)positions, (void*)sequence, (void*)plan);
+        return false;
+      }
   const int smem = (n + kWaves + p.blocks()) * (int)sizeof(int);
   static LdsLimit lds;
   if (!lds.allow(packed_plan_kernel, (kMaxSequences + kWaves + kMaxRows / kPlanBlock) * (int)sizeof(int))) return false;

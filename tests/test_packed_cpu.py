@@ -30,6 +30,18 @@ def test_plan_refuses(lengths, n, rows, plan):
     _refused(po.po_op_packed_plan, "packed_plan", lengths, n, rows, None, None, None, plan, stream=0)
 
 
+OVERLAPS = [dict(starts=AT), dict(starts=AT - 16), dict(positions=AT + 8), dict(sequence=AT), dict(plan=AT), dict(starts=AT + 64, positions=AT + 72),
+            dict(positions=AT + 64, sequence=AT + 64), dict(positions=AT + 64, plan=AT + 80), dict(starts=AT + 1024, plan=AT + 48)]
+ASKEW = [dict(starts=AT + 66), dict(positions=AT + 65), dict(sequence=AT + 67), dict(lengths=AT + 2)]
+
+
+@pytest.mark.parametrize("given", OVERLAPS + ASKEW, ids=[str(i) for i in range(13)])
+def test_plan_refuses_arrays_that_overlap_or_lie_askew(given):
+    """4 lengths at AT, 8 rows."""
+    c = {**dict(lengths=AT, starts=None, positions=None, sequence=None, plan=None), **given}
+    _refused(po.po_op_packed_plan, "none overlaps", c["lengths"], 4, 8, c["starts"], c["positions"], c["sequence"], c["plan"], stream=0)
+
+
 GOOD = dict(qkv=AT, plan=AT, o=AT, lse=AT, d_o=AT, dqkv=AT, workspace=AT, rows=100, h=256, n_heads=4, n_kv_heads=2)
 BAD_SHAPES = [dict(rows=0), dict(rows=-1), dict(rows=2097153), dict(h=0), dict(n_heads=0), dict(n_heads=-4), dict(n_heads=3), dict(n_kv_heads=3),
               dict(n_kv_heads=8), dict(h=128), dict(h=384), dict(h=1024), dict(h=2 ** 30, n_heads=2 ** 24, n_kv_heads=1),
