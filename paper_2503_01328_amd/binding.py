@@ -146,11 +146,17 @@ def _ptr(t):
     return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
+# Not part of torch's public interface: None where a torch has it no more.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     """Raw handle of a torch stream, an int, or None: the current stream of the current device, whose handle alone takes a
     sixth of the time that torch.cuda.current_stream() needs to make an object of it (2.8 of the 7.1 us of a small launch)."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        stream = torch.cuda.current_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -4,6 +4,7 @@ validation) agree with the independent oracle models.  No GPU work is issued."""
 import ctypes
 import os
 import re
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -404,3 +405,14 @@ def test_trace_viewer_reads_the_span_file(tmp_path):
     assert "run of 4.00 ms, 3 spans" in text and "compute: 2 spans, busy 2.50 ms" in text
     assert "H2D: 1 spans, busy 3.00 ms" in text and "gap  0.50" in text
     assert trace.main(["trace", str(f), "0"]) == 0 and trace.main(["trace"]) == 2
+
+
+def test_current_stream_with_and_without_torchs_raw_handle(monkeypatch):
+    """The binding asks torch for the current stream's handle by a function that is not public, and does without where there is none."""
+    monkeypatch.setattr(po.torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(po, "_raw_stream", lambda device: 100 + device)
+    assert po._stream(None) == 103
+    monkeypatch.setattr(po, "_raw_stream", None)
+    monkeypatch.setattr(po.torch.cuda, "current_stream", lambda: SimpleNamespace(cuda_stream=77))
+    assert po._stream(None) == 77
+    assert po._stream(5) == 5 and po._stream(SimpleNamespace(cuda_stream=9)) == 9

@@ -588,6 +588,12 @@ def test_on_two_streams_at_once(gpu_device):
         assert all(torch.equal(x, y) for x, y in zip(layer.results(), want))
 
 
+def test_calls_without_a_stream_go_to_the_current_one(gpu_device):
+    for stream in (torch.cuda.current_stream(), torch.cuda.Stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            assert po._stream(None) == torch.cuda.current_stream().cuda_stream == stream.cuda_stream
+
+
 def test_inputs_are_left_alone(gpu_device):
     layer = _Layer(gpu_device, "bf16", 200, 64, 4, 2, [90, 100])
     kept = [t.clone() for t in (layer.lengths, layer.qkv, layer.d_o, layer.gains, layer.inv_freq)]
