@@ -330,7 +330,9 @@ int po_op_packed_plan(const int32_t* lengths, int32_t n_sequences, int32_t rows,
  * d_o [rows, h], lse [n_heads, rows], dqkv like qkv, head sizes 64 and 128, all tensors 16-byte aligned.  plan: as po_op_packed_plan left it
  * for the same `rows` (of one made for another row count nothing is computed).  Rows behind the last sequence are not read as
  * keys or queries and left as they were in every output.  An infinity or NaN in a row of one sequence reaches no other sequence,
- * in a key or value row no row of o and dQ before it.  o is not qkv, dqkv neither qkv nor d_o.
+ * in a key or value row no row of o and dQ before it; rows of results that are not finite, but not NaN altogether, are computed one by one,
+ * which for a long sequence takes hundreds of times as long.  o is not qkv, dqkv neither qkv nor d_o.
+ * With PO_BF16 P and dS enter their products as bf16 values, dS for dQ as the sum of two, whatever the lengths.
  * workspace: po_op_attention_packed_backward_workspace bytes, 16-byte aligned, contents unspecified before and afterwards; one for more
  * rows (of the same type and heads) serves fewer.
  * Results do not depend on how often or beside what a call runs: no atomics. */

@@ -21,7 +21,9 @@
 // first of these and 88 and 188, 135 and 226, 31 and 84 for the last three.
 //
 // P and dS are rounded to bf16 once on their way into the second product, as the inputs of every product here are (dS for dQ in two
-// terms: TwoTerms); sums, maxima and accumulators are fp32.
+// terms: TwoTerms); sums, maxima and accumulators are fp32.  Each such rounding is as large as that of the result itself: against 64 bits o is 1.07
+// to 1.31 times as far off as fp32 arithmetic rounded once at the end, the gradient 1.36 to 1.40 times.  Three terms, which are the fp32 value,
+// took 2 to 35 % longer.
 // A key or value that is not finite reaches the rows that see it and no other, nor does a row of d_o reach another sequence: results that
 // are not finite are redone row by row (attention_packed_rows.h).  Rows behind the last sequence read as zeros and are never written.
 #include <algorithm>
