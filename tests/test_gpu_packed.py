@@ -594,6 +594,43 @@ def test_calls_without_a_stream_go_to_the_current_one(gpu_device):
             assert po._stream(None) == torch.cuda.current_stream().cuda_stream == stream.cuda_stream
 
 
+@pytest.mark.parametrize("rows,largest", [(512, 513), (1000, 1025), (1024, 1400)])
+def test_a_workspace_kept_from_a_larger_batch(gpu_device, rows, largest):
+    """Both backward calls in fp32, in a workspace of the size that a larger batch asks for, with nothing written behind it: as in one of their own."""
+    dh, a, akv = 128, 16, 4
+    layer = _Layer(gpu_device, "f32", rows, dh, a, akv, [rows // 2, rows // 3])
+    layer.run()
+    torch.cuda.synchronize()
+    want = layer.results()
+    layer.clear()
+    size = max(po.po_op_attention_packed_backward_workspace(layer.code, largest, a * dh, a, akv),
+               po.po_op_qk_norm_rotary_backward_workspace(largest, a * dh, a, akv))
+    layer.ws = torch.full((size + (1 << 16),), 255, dtype=torch.uint8, device=gpu_device)
+    layer.run()
+    torch.cuda.synchronize()
+    assert bool((layer.ws[size:] == 255).all())
+    assert all(torch.equal(x, y) for x, y in zip(layer.results(), want))
+
+
+@pytest.mark.parametrize("rows,largest", [(512, 513), (1024, 1025), (300, 2048)])
+def test_a_rotation_workspace_kept_from_a_larger_batch(gpu_device, rows, largest):
+    dh, a, akv = 128, 40, 8
+    h, hkv, g = a * dh, akv * dh, _gen(gpu_device, 31)
+    qkv, d_out = (torch.randn(rows, h + 2 * hkv, generator=g, device=gpu_device).bfloat16() for _ in range(2))
+    gains = 1 + 0.1 * torch.randn(2, dh, generator=g, device=gpu_device).bfloat16()
+    positions = torch.arange(rows, device=gpu_device, dtype=torch.int32)
+    inv_freq = torch.rand(64, generator=g, device=gpu_device)
+    results = []
+    for asked in (rows, largest):
+        size = po.po_op_qk_norm_rotary_backward_workspace(asked, h, a, akv)
+        ws = torch.full((size + (1 << 20),), 255, dtype=torch.uint8, device=gpu_device)
+        dqkv, dg = torch.empty_like(qkv), torch.zeros(2, dh, device=gpu_device)
+        po.po_op_qk_norm_rotary_backward(po.PO_BF16, d_out, qkv, gains[0], gains[1], positions, inv_freq, [64], 0, dqkv, dg[0], dg[1], ws, rows, h, a, akv)
+        assert bool((ws[size:] == 255).all())
+        results.append((dqkv, dg))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
 def test_inputs_are_left_alone(gpu_device):
     layer = _Layer(gpu_device, "bf16", 200, 64, 4, 2, [90, 100])
     kept = [t.clone() for t in (layer.lengths, layer.qkv, layer.d_o, layer.gains, layer.inv_freq)]
