@@ -396,6 +396,69 @@ int po_op_colsum_accumulate_static(int32_t dtype, const void* x, float* acc, int
 int po_op_pack(const void* const* seg_ptrs, const uint64_t* seg_bytes, int32_t n_seg, void* packed, void* stream);
 int po_op_unpack(void* const* seg_ptrs, const uint64_t* seg_bytes, int32_t n_seg, const void* packed, void* stream);
 
+/* 8-bit checkpoints: what a layer saves for its backward pass at 33/32 bytes a value, so that half the bytes of a bf16 saved set (a quarter of
+ * an fp32 one) stay resident or travel to the host (Section 4.2's volume; one contiguous buffer a tensor, a segment for po_op_pack).  Lossy: for
+ * callers who choose it; the stage itself saves what it computed.
+ *
+ * The checkpoint of a tensor [rows, cols] is a buffer of po_op_saved8_bytes(rows, cols) bytes (a multiple of 16), 16-byte aligned: codes uint8
+ * [rows, C], C = cols rounded up to 32 (zeros behind the last column), then scale bytes uint8 [rows, C / 32].  A block is 32 consecutive columns of a row.
+ * Its exponent e is the least integer, at least -117, for which its largest finite magnitude is at most 448 * 2^e; the scale byte is e + 127, a
+ * code the e4m3 number (OCP, no infinities) nearest to x / 2^e, ties to even: off by at most 2^-4 of the value, or 2^-10 * 2^e.  A restored value, code * 2^e,
+ * is exact in bf16 and fp32.  NaN and infinities are restored as NaN, magnitudes over 1.875 * 2^127 as that.  Up to 2^31 values, padding included
+ * (beyond: PO_E_INVAL, and 0 bytes).
+ *
+ * po_op_save8 / po_op_restore8: n (1 to 8) tensors of dtype in one launch.  All arrays are HOST arrays of length n: x DEVICE pointers, ld their row
+ * strides in elements (at least cols, so that columns of a wider tensor can be saved and restored), saved DEVICE pointers.  What is written
+ * overlaps nothing else (PO_E_INVAL).  A checkpoint may be restored in the other dtype. */
+uint64_t po_op_saved8_bytes(int32_t rows, int32_t cols);
+int po_op_save8(int32_t dtype, int32_t n, const void* const* x, const int32_t* rows, const int32_t* cols, const int32_t* ld,
+                void* const* saved, void* stream);
+int po_op_restore8(int32_t dtype, int32_t n, const void* const* saved, const int32_t* rows, const int32_t* cols, const int32_t* ld,
+                   void* const* x, void* stream);
+
+/* A feed-forward's activation: out [rows, f] = act(u), u [rows, f], or gated, out = act(a) * b, u [rows, 2 f] = a | b.  act: a po_activation (GeLU in the
+ * tanh form of the stage).  saved_u: NULL, or the checkpoint of u, written in the same pass.  out may be u where there is no gate. */
+typedef enum { PO_ACT_GELU = 0, PO_ACT_SILU = 1 } po_activation;
+int po_op_activation_forward(int32_t dtype, int32_t act, int32_t gated, const void* u, void* out, void* saved_u, int32_t rows, int32_t f,
+                             void* stream);
+/* du (like u) from d_out [rows, f], u its checkpoint (u_saved8 not 0) or the tensor of dtype.  out: NULL, or act(a) (* b) again, which the
+ * gradient of the weight behind needs.  du may be d_out where there is no gate. */
+int po_op_activation_backward(int32_t dtype, int32_t act, int32_t gated, const void* u, int32_t u_saved8, const void* d_out, void* du,
+                              void* out, int32_t rows, int32_t f, void* stream);
+
+/* A block's output f on its way into the residual stream x, and the norm in front of the next block, all [rows, h] of dtype:
+ *   z = N(f) * post_gain + post_shift (post_gain NULL: z = f),  y = skip * x + branch * gate * z (gate NULL: 1),
+ *   n = N(y) * pre_gain + pre_shift (pre_gain and n NULL: no norm there)
+ * N, a po_norm for both: (v - mean) / sqrt(var + eps) over a row, biased variance, or v / sqrt(mean(v^2) + eps), which has no shifts.  Gains and
+ * shifts [h] of dtype, a shift may be NULL.  gate of dtype: [h] (gate_per_value 0) or [rows, h] (1).  saved_f, saved_y: NULL, or the checkpoints of f and
+ * of y as it is stored.  y may be x, n may be f; what is written overlaps nothing else.  h 1 to 16384, 1 to 2^25 rows.
+ * With post_gain and gate NULL and scales of 1 this is a layer's residual sum and LayerNorm. */
+typedef enum { PO_NORM_LAYER = 0, PO_NORM_RMS = 1 } po_norm;
+int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const void* f, const void* post_gain, const void* post_shift,
+                            const void* gate, int32_t gate_per_value, float skip, float branch, const void* pre_gain, const void* pre_shift,
+                            void* y, void* n, void* saved_f, void* saved_y, int32_t rows, int32_t h, float eps, void* stream);
+/* dx and df [rows, h], the gradients of x and f, from dy and dn, those of y and n (dy may be NULL for none; dn NULL: no norm of y, pre_gain NULL too).
+ * y and f: checkpoints (y_saved8, f_saved8 not 0) or tensors of dtype; y is read where dn is given, f where post_gain or gate is (else NULL
+ * will do).  A gradient for every parameter that is given and no other: dpost_gain, dpost_shift, dpre_gain, dpre_shift fp32 [h] +=, in a fixed
+ * order; dgate fp32 [h] += for a gate [h], of dtype [rows, h] for one per value.  n: NULL, or n again from y, which the gradient of the weight
+ * behind needs.  dx may be dy, df may be dn; what is written overlaps nothing else.  workspace: 16-byte aligned,
+ * po_op_norm_join_backward_workspace bytes, contents unspecified before and afterwards; one for more rows (of the same h) serves fewer; NULL where
+ * no sum is wanted. */
+uint64_t po_op_norm_join_backward_workspace(int32_t rows, int32_t h);
+int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const void* dn, const void* y, int32_t y_saved8, const void* f,
+                             int32_t f_saved8, const void* post_gain, const void* post_shift, const void* gate, int32_t gate_per_value,
+                             float skip, float branch, const void* pre_gain, const void* pre_shift, void* dx, void* df, void* dgate,
+                             float* dpost_gain, float* dpost_shift, float* dpre_gain, float* dpre_shift, void* n, void* workspace,
+                             int32_t rows, int32_t h, float eps, void* stream);
+
+/* A weight's gradient from the checkpoint of its input: dw [k, n] fp32 (row stride ldc) = X^T dY (accumulate 0) or += (1), X [rows, k] as saved_x holds it,
+ * dy [rows, n] of dtype (row stride ldy).  Exact products, fp32 sums, whatever dtype is, in an order that depends on the sizes alone.  dw overlaps neither
+ * input.  workspace: po_op_weight_grad_saved8_workspace bytes (often 0: NULL will do), 16-byte aligned, contents unspecified before and
+ * afterwards; one for more rows (of the same dtype, k and n) serves fewer.  1 to 2^25 rows, k and n 1 to 2^20 (beyond: PO_E_INVAL, and 0 bytes). */
+uint64_t po_op_weight_grad_saved8_workspace(int32_t dtype, int32_t rows, int32_t k, int32_t n);
+int po_op_weight_grad_saved8(int32_t dtype, const void* saved_x, const void* dy, int32_t ldy, float* dw, int32_t ldc, int32_t accumulate,
+                             void* workspace, int32_t rows, int32_t k, int32_t n, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

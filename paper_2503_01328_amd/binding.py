@@ -27,6 +27,8 @@ PO_SCHED_1F1B, PO_SCHED_1F1B_INTERLEAVED, PO_SCHED_GIS, PO_SCHED_PO = 0, 1, 2, 3
 PO_SEL_ALTERNATE_MB, PO_SEL_LONGEST_LIFESPAN = 0, 1
 PO_OK, PO_E_INVAL, PO_E_STATE, PO_E_DEVICE_OOM, PO_E_HOST_OOM, PO_E_HIP = 0, -1, -2, -3, -4, -5
 PO_ROTARY_HALVES, PO_ROTARY_NEIGHBOURS = 0, 1
+PO_ACT_GELU, PO_ACT_SILU = 0, 1
+PO_NORM_LAYER, PO_NORM_RMS = 0, 1
 OP_KINDS = ("F", "B", "OFFLOAD", "RELOAD", "W")
 
 
@@ -119,6 +121,19 @@ EXPORTS = {
     "po_op_colsum_accumulate_static": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
     "po_op_pack": (C.c_int, [C.POINTER(C.c_void_p), C.POINTER(C.c_uint64), C.c_int32, C.c_void_p, C.c_void_p]),
     "po_op_unpack": (C.c_int, [C.POINTER(C.c_void_p), C.POINTER(C.c_uint64), C.c_int32, C.c_void_p, C.c_void_p]),
+    "po_op_saved8_bytes": (C.c_uint64, [C.c_int32, C.c_int32]),
+    "po_op_save8": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_void_p)] + [C.POINTER(C.c_int32)] * 3 + [C.POINTER(C.c_void_p), C.c_void_p]),
+    "po_op_restore8": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_void_p)] + [C.POINTER(C.c_int32)] * 3 + [C.POINTER(C.c_void_p), C.c_void_p]),
+    "po_op_activation_forward": (C.c_int, [C.c_int32] * 3 + [C.c_void_p] * 3 + [C.c_int32, C.c_int32, C.c_void_p]),
+    "po_op_activation_backward": (C.c_int, [C.c_int32] * 3 + [C.c_void_p, C.c_int32] + [C.c_void_p] * 3 + [C.c_int32, C.c_int32, C.c_void_p]),
+    "po_op_norm_join_forward": (C.c_int, [C.c_int32] * 2 + [C.c_void_p] * 5 + [C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 6 +
+                                [C.c_int32, C.c_int32, C.c_float, C.c_void_p]),
+    "po_op_norm_join_backward_workspace": (C.c_uint64, [C.c_int32, C.c_int32]),
+    "po_op_norm_join_backward": (C.c_int, [C.c_int32] * 2 + [C.c_void_p] * 3 + [C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 3 +
+                                 [C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 11 + [C.c_int32, C.c_int32, C.c_float, C.c_void_p]),
+    "po_op_weight_grad_saved8_workspace": (C.c_uint64, [C.c_int32] * 4),
+    "po_op_weight_grad_saved8": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p] +
+                                 [C.c_int32] * 3 + [C.c_void_p]),
 }
 for _name, (_res, _args) in EXPORTS.items():
     _f = getattr(lib, _name)
@@ -403,3 +418,73 @@ def po_op_unpack(segments, packed, stream=None):
     ptrs = (C.c_void_p * len(segments))(*[(s if isinstance(s, int) else s.data_ptr()) for s, _ in segments])
     sizes = (C.c_uint64 * len(segments))(*[b for _, b in segments])
     _check(lib.po_op_unpack(ptrs, sizes, len(segments), _ptr(packed), _stream(stream)))
+
+
+def po_op_saved8_bytes(rows, cols) -> int:
+    return lib.po_op_saved8_bytes(rows, cols)
+
+
+def _matrices(tensors):
+    """[(pointer, rows, cols, row stride)] of 2-d tensors with neighbouring columns, or of such tuples, as C arrays."""
+    given = []
+    for t in tensors:
+        if not isinstance(t, tuple):
+            rows, cols = t.shape
+            if cols > 1 and t.stride(1) != 1:
+                raise ValueError("the columns of a row have to be neighbours")
+            t = (t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols)
+        given.append(t)
+    n = len(given)
+    return n, (C.c_void_p * n)(*[g[0] for g in given]), *((C.c_int32 * n)(*[g[k] for g in given]) for k in (1, 2, 3))
+
+
+def po_op_save8(dtype, tensors, saved, stream=None):
+    """tensors: list of 2-d tensors (rows may have a stride) or (pointer, rows, cols, row stride); saved: their checkpoints' buffers."""
+    n, x, rows, cols, ld = _matrices(tensors)
+    if len(saved) != n:
+        raise ValueError("a checkpoint for every tensor is needed")
+    _check(lib.po_op_save8(dtype, n, x, rows, cols, ld, (C.c_void_p * n)(*[_ptr(s) for s in saved]), _stream(stream)))
+
+
+def po_op_restore8(dtype, saved, tensors, stream=None):
+    """saved, tensors: as for po_op_save8."""
+    n, x, rows, cols, ld = _matrices(tensors)
+    if len(saved) != n:
+        raise ValueError("a checkpoint for every tensor is needed")
+    _check(lib.po_op_restore8(dtype, n, (C.c_void_p * n)(*[_ptr(s) for s in saved]), rows, cols, ld, x, _stream(stream)))
+
+
+def po_op_activation_forward(dtype, act, gated, u, out, saved_u, rows, f, stream=None):
+    _check(lib.po_op_activation_forward(dtype, act, gated, _ptr(u), _ptr(out), _ptr(saved_u), rows, f, _stream(stream)))
+
+
+def po_op_activation_backward(dtype, act, gated, u, u_saved8, d_out, du, out, rows, f, stream=None):
+    _check(lib.po_op_activation_backward(dtype, act, gated, _ptr(u), u_saved8, _ptr(d_out), _ptr(du), _ptr(out), rows, f, _stream(stream)))
+
+
+def po_op_norm_join_forward(dtype, norm, x, f, post_gain, post_shift, gate, gate_per_value, skip, branch, pre_gain, pre_shift, y, n, saved_f,
+                            saved_y, rows, h, eps, stream=None):
+    _check(lib.po_op_norm_join_forward(dtype, norm, _ptr(x), _ptr(f), _ptr(post_gain), _ptr(post_shift), _ptr(gate), gate_per_value, skip, branch,
+                                       _ptr(pre_gain), _ptr(pre_shift), _ptr(y), _ptr(n), _ptr(saved_f), _ptr(saved_y), rows, h, eps,
+                                       _stream(stream)))
+
+
+def po_op_norm_join_backward_workspace(rows, h) -> int:
+    return lib.po_op_norm_join_backward_workspace(rows, h)
+
+
+def po_op_norm_join_backward(dtype, norm, dy, dn, y, y_saved8, f, f_saved8, post_gain, post_shift, gate, gate_per_value, skip, branch, pre_gain,
+                             pre_shift, dx, df, dgate, dpost_gain, dpost_shift, dpre_gain, dpre_shift, n, workspace, rows, h, eps, stream=None):
+    _check(lib.po_op_norm_join_backward(dtype, norm, _ptr(dy), _ptr(dn), _ptr(y), y_saved8, _ptr(f), f_saved8, _ptr(post_gain), _ptr(post_shift),
+                                        _ptr(gate), gate_per_value, skip, branch, _ptr(pre_gain), _ptr(pre_shift), _ptr(dx), _ptr(df), _ptr(dgate),
+                                        _ptr(dpost_gain), _ptr(dpost_shift), _ptr(dpre_gain), _ptr(dpre_shift), _ptr(n), _ptr(workspace), rows,
+                                        h, eps, _stream(stream)))
+
+
+def po_op_weight_grad_saved8_workspace(dtype, rows, k, n) -> int:
+    return lib.po_op_weight_grad_saved8_workspace(dtype, rows, k, n)
+
+
+def po_op_weight_grad_saved8(dtype, saved_x, dy, ldy, dw, ldc, accumulate, workspace, rows, k, n, stream=None):
+    _check(lib.po_op_weight_grad_saved8(dtype, _ptr(saved_x), _ptr(dy), ldy, _ptr(dw), ldc, accumulate, _ptr(workspace), rows, k, n,
+                                        _stream(stream)))

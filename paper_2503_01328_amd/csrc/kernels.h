@@ -192,6 +192,38 @@ size_t qk_norm_rotary_backward_workspace(int rows, int h, int n_heads);
 bool qk_norm_rotary_backward(int dtype, const QkNormRotary& a, const void* d_out, const void* qkv, void* dqkv, float* dgain_q,
                              float* dgain_k, float* workspace, hipStream_t stream);
 
+// ---- 8-bit checkpoints (saved8.hip, activation.hip, norm_join.hip, weight_grad_saved8.hip) ------------------------------
+constexpr int kMaxSaved8Tensors = 8;
+constexpr int64_t kMaxSaved8Chunks = 1 << 28;  // eights of values of a tensor: 2^31 values
+bool save8(int dtype, int n, const void* const* x, const int* rows, const int* cols, const int* ld, void* const* saved, hipStream_t stream);
+bool restore8(int dtype, int n, const void* const* saved, const int* rows, const int* cols, const int* ld, void* const* x, hipStream_t stream);
+constexpr int kActGelu = 0, kActSilu = 1, kNormLayer = 0, kNormRms = 1;
+bool activation_forward(int dtype, int act, int gated, const void* u, void* out, void* saved_u, int rows, int f, hipStream_t stream);
+bool activation_backward(int dtype, int act, int gated, const void* u, int u_saved8, const void* d_out, void* du, void* out, int rows, int f,
+                         hipStream_t stream);
+struct NormJoin {
+  int norm;
+  const void *post_gain, *post_shift, *gate, *pre_gain, *pre_shift;  // of dtype; null: not there
+  int gate_per_value;
+  float skip, branch;
+  int rows, h;
+  float eps;
+};
+struct NormJoinBackward {
+  const void *dy, *dn, *y, *f;
+  int y_saved8, f_saved8;
+  void *dx, *df, *dgate, *n;
+  float *dpost_gain, *dpost_shift, *dpre_gain, *dpre_shift;
+  void* workspace;
+};
+bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* f, void* y, void* n, void* saved_f, void* saved_y,
+                       hipStream_t stream);
+size_t norm_join_backward_workspace(int rows, int h);
+bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream);
+size_t weight_grad_saved8_workspace(int rows, int k, int n);
+bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy, float* dw, int ldc, int accumulate, void* workspace, int rows,
+                        int k, int n, hipStream_t stream);
+
 #define PO_HIP_OK(expr)                                                                  \
   do {                                                                                   \
     hipError_t e__ = (expr);                                                             \

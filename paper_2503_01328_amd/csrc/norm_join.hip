@@ -1,0 +1,605 @@
+// A block's output on its way back into the residual stream, and the norm in front of the next block:
+//
+//   z = N(f) gain2 + shift2 (or f),  y = skip x + branch g z (g: none, one for each column, one for each value),  n = N(y) gain + shift
+// N: LayerNorm, (v - mean) / sqrt(var + eps), or the RMS norm, v / sqrt(mean(v^2) + eps).  The forward leaves 8-bit checkpoints of f and y
+// (saved8.h), y's of y as it is stored.  Backward, from dy and dn, f and y (checkpoints or tensors):
+//   a = dn gain,  t = dy + r (a - mean(a) - yh mean(a yh))  (yh = N(y), r its root; RMS: without mean(a)),  dx = skip t
+//   w = branch t,  dg = w z,  dz = w g,  b = dz gain2,  df = r2 (b - mean(b) - fh mean(b fh))
+//   dgain += sum dn yh, dshift += sum dn, dgain2 += sum dz fh, dshift2 += sum dz, and dg's sum where g is one for each column
+// n can be had again beside: it is the input of the weight gradient that follows.  Everything between the loads and the one rounding of a
+// store is fp32, variances are those of centred values.
+//
+// Bound by memory: every tensor once.  A block of as many waves as a row of eights needs takes a row, values stay in registers from
+// the load to the store, sums go over the lanes by lane exchanges and over the waves through LDS.  Backward blocks take rows one after another and
+// hold their columns' sums of the parameter gradients in registers; a second launch adds the blocks' in a fixed order: no atomics.
+#include <algorithm>
+
+#include "saved8.h"
+
+namespace po {
+
+namespace {
+
+constexpr int kMaxWaves = 16, kMaxWidth = kMaxWaves * 64 * 8 * 2, kMaxRows = 1 << 25;
+constexpr int kMaxBlocks = 512;  // of the backward: each leaves a partial sum of every parameter's gradient
+
+struct Join {
+  const void *x, *f, *gate, *post_gain, *post_shift, *pre_gain, *pre_shift;
+  const void *dy, *dn, *y_in;
+  const uint8_t *f_codes, *y_codes;  // backward: the checkpoints, where f and y_in are null
+  uint8_t *f_codes_out, *y_codes_out;
+  void *y, *n, *dx, *df, *dgate;
+  float* partials;
+  int rows, h, padded, vec, gate_per_value, layer;
+  float skip, branch, eps;
+};
+
+// Sum over a wave, the same in every lane: rows of 16 lanes by exchanges, then the four rows.
+__device__ __forceinline__ float sum_of_wave(float v) {
+#define PO_ADD_DPP(ctrl) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true))
+  PO_ADD_DPP(0xb1);   // neighbours
+  PO_ADD_DPP(0x4e);   // pairs of four
+  PO_ADD_DPP(0x141);  // half rows mirrored
+  PO_ADD_DPP(0x140);  // rows mirrored
+#undef PO_ADD_DPP
+  auto row = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
+// Sums of N values over the block.  Two buffers in turn: who writes one has passed the barrier behind the other's reads.
+struct BlockSums {
+  float (*room)[4][kMaxWaves];
+  int turn = 0, waves;
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = sum_of_wave(v[k]);
+    if (waves == 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float(*r)[kMaxWaves] = room[turn];
+    turn ^= 1;
+    if (lane == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) r[k][wave] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float s = 0.f;
+      for (int w = 0; w < waves; ++w) s += r[k][w];
+      v[k] = s;
+    }
+  }
+};
+
+// A lane's columns: eights waves * 64 lanes apart.  held: how many of an eight's columns there are.
+struct Lane {
+  int col[2], held[2];
+  bool whole[2], padded[2];  // all eight, 16-byte loads; a chunk of the checkpoint
+};
+template <int C>
+__device__ __forceinline__ Lane lane_of(const Join& p) {
+  Lane l;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    l.col[c] = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    l.held[c] = p.h - l.col[c];
+    l.whole[c] = p.vec && l.held[c] >= 8;
+    l.padded[c] = l.col[c] < p.padded;
+  }
+  return l;
+}
+template <int C>
+__device__ __forceinline__ void clear(float (&v)[C][8]) {
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
+}
+template <typename T, int C>
+__device__ __forceinline__ void load_row(float (&v)[C][8], const void* p, int64_t row, int h, const Lane& l) {
+#pragma unroll
+  for (int c = 0; c < C; ++c) load_eight(v[c], (const T*)p + row * h + l.col[c], l.held[c], l.whole[c]);
+}
+template <typename T, int C>
+__device__ __forceinline__ void store_row(void* p, const float (&v)[C][8], int64_t row, int h, const Lane& l) {
+#pragma unroll
+  for (int c = 0; c < C; ++c) store_eight((T*)p + row * h + l.col[c], v[c], l.held[c], l.whole[c]);
+}
+// A row of a checkpoint, zeros behind its last column.
+template <int C>
+__device__ __forceinline__ void load_saved(float (&v)[C][8], const uint8_t* codes, int64_t row, const Join& p, const Lane& l) {
+  const uint8_t* scales = codes + (int64_t)p.rows * p.padded;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    uint2 q = make_uint2(0, 0);
+    unsigned byte = 127;
+    if (l.held[c] > 0) {
+      const int64_t at = row * p.padded + l.col[c];
+      q = *(const uint2*)(codes + at);
+      byte = scales[at / 32];
+    }
+    saved8_decode(q, byte, v[c]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= l.held[c]) v[c][i] = 0.f;
+  }
+}
+template <int C>
+__device__ __forceinline__ void save_row(uint8_t* codes, const float (&v)[C][8], int64_t row, const Join& p, const Lane& l) {
+  uint8_t* scales = codes + (int64_t)p.rows * p.padded;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    unsigned byte;
+    const uint2 q = saved8_encode(v[c], byte);
+    if (l.padded[c]) {
+      const int64_t at = row * p.padded + l.col[c];
+      *(uint2*)(codes + at) = q;
+      if (threadIdx.x % 4 == 0) scales[at / 32] = (uint8_t)byte;
+    }
+  }
+}
+template <int C>
+__device__ __forceinline__ float sum_of(const float (&v)[C][8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += v[c][i];
+  return s;
+}
+template <int C>
+__device__ __forceinline__ float dot_of(const float (&v)[C][8], const float (&w)[C][8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(v[c][i], w[c][i], s);
+  return s;
+}
+// v - mean where there is a column, zero elsewhere.
+template <int C>
+__device__ __forceinline__ void centre(float (&v)[C][8], float mean, const Lane& l) {
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] = i < l.held[c] ? v[c][i] - mean : 0.f;
+}
+
+// v becomes N(v).
+template <int C>
+__device__ __forceinline__ void normalise(float (&v)[C][8], const Join& p, const Lane& l, BlockSums& sums) {
+  float s[1];
+  const float over_h = 1.f / (float)p.h;
+  if (p.layer) {
+    s[0] = sum_of(v);
+    sums(s);
+    centre(v, s[0] * over_h, l);
+  }
+  s[0] = dot_of(v, v);
+  sums(s);
+  const float r = rsqrtf(s[0] * over_h + p.eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] *= r;
+}
+template <typename T, int C>
+__device__ __forceinline__ void affine(float (&v)[C][8], const void* gain, const void* shift, const Lane& l) {
+  float w[C][8];
+  load_row<T>(w, gain, 0, 0, l);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] *= w[c][i];
+  if (!shift) return;
+  load_row<T>(w, shift, 0, 0, l);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] += w[c][i];
+}
+
+template <typename T, int C>
+__global__ __launch_bounds__(1024) void norm_join_forward_kernel(Join p) {
+  __shared__ float room[2][4][kMaxWaves];
+  const Lane l = lane_of<C>(p);
+  BlockSums sums{room, 0, (int)blockDim.x >> 6};
+  const int64_t row = blockIdx.x;
+  float f[C][8], x[C][8], g[C][8];
+  load_row<T>(f, p.f, row, p.h, l);
+  load_row<T>(x, p.x, row, p.h, l);
+  if (p.gate) load_row<T>(g, p.gate, p.gate_per_value ? row : 0, p.h, l);
+  if (p.f_codes_out) save_row(p.f_codes_out, f, row, p, l);
+  if (p.post_gain) {
+    normalise(f, p, l, sums);
+    affine<T>(f, p.post_gain, p.post_shift, l);
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float z = p.gate ? f[c][i] * g[c][i] : f[c][i];
+      x[c][i] = fmaf(p.skip, x[c][i], p.branch * z);
+    }
+  store_row<T>(p.y, x, row, p.h, l);
+  if (p.y_codes_out) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[c][i] = to_f32(from_f32<T>(x[c][i]));
+    save_row(p.y_codes_out, f, row, p, l);
+  }
+  if (!p.pre_gain) return;
+  normalise(x, p, l, sums);
+  affine<T>(x, p.pre_gain, p.pre_shift, l);
+  store_row<T>(p.n, x, row, p.h, l);
+}
+
+// Which sums a block leaves, in this order.
+enum Sum { kPreGain, kPreShift, kPostGain, kPostShift, kGate, kSums };
+struct SumTargets {
+  float* to[kSums];  // null: not among the partial sums
+};
+
+// POST: there is a norm of f; COLUMNS: a gate for each column, whose gradient is a sum.
+template <typename T, int C, bool LAYER, bool POST, bool COLUMNS>
+__global__ __launch_bounds__(1024) void norm_join_backward_kernel(Join p) {
+  __shared__ float room[2][4][kMaxWaves];
+  const Lane l = lane_of<C>(p);
+  BlockSums sums{room, 0, (int)blockDim.x >> 6};
+  const float over_h = 1.f / (float)p.h;
+  float dpre_gain[C][8], dpre_shift[C][8], dpost_gain[C][8], dpost_shift[C][8], dgate[C][8];
+  clear(dpre_gain);
+  clear(dpre_shift);
+  clear(dpost_gain);
+  clear(dpost_shift);
+  clear(dgate);
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    float t[C][8], y[C][8], d[C][8], f[C][8], g[C][8];
+    if (p.dy) load_row<T>(t, p.dy, row, p.h, l);
+    else clear(t);
+    const bool uses_f = POST || p.gate;
+    if (p.dn) {
+      load_row<T>(d, p.dn, row, p.h, l);
+      if (p.y_codes) load_saved(y, p.y_codes, row, p, l);
+      else load_row<T>(y, p.y_in, row, p.h, l);
+    }
+    if (uses_f) {
+      if (p.f_codes) load_saved(f, p.f_codes, row, p, l);
+      else load_row<T>(f, p.f, row, p.h, l);
+    }
+    if (p.gate) load_row<T>(g, p.gate, p.gate_per_value ? row : 0, p.h, l);
+
+    float rf = 1.f;
+    if (p.dn || POST) {  // both norms' statistics
+      float s[2] = {0.f, 0.f};
+      if (LAYER) {
+        if (p.dn) s[0] = sum_of(y);
+        if (POST) s[1] = sum_of(f);
+        sums(s);
+        if (p.dn) centre(y, s[0] * over_h, l);
+        if (POST) centre(f, s[1] * over_h, l);
+      }
+      s[0] = p.dn ? dot_of(y, y) : 0.f;
+      s[1] = POST ? dot_of(f, f) : 0.f;
+      sums(s);
+      rf = rsqrtf(s[1] * over_h + p.eps);
+      if (POST) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[c][i] *= rf;
+      }
+      if (p.dn) {
+        const float r = rsqrtf(s[0] * over_h + p.eps);
+        float w[C][8];
+        load_row<T>(w, p.pre_gain, 0, 0, l);
+        float m[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            y[c][i] *= r;
+            dpre_gain[c][i] = fmaf(d[c][i], y[c][i], dpre_gain[c][i]);
+            if (LAYER) dpre_shift[c][i] += d[c][i];
+            d[c][i] *= w[c][i];
+            if (LAYER) m[0] += d[c][i];
+            m[1] = fmaf(d[c][i], y[c][i], m[1]);
+          }
+        sums(m);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) t[c][i] = fmaf(r, d[c][i] - m[0] * over_h - y[c][i] * (m[1] * over_h), t[c][i]);
+        if (p.n) {
+          affine<T>(y, p.pre_gain, p.pre_shift, l);
+          store_row<T>(p.n, y, row, p.h, l);
+        }
+      }
+    }
+    // what f's branch gets
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[c][i] = p.branch * t[c][i];
+        t[c][i] *= p.skip;
+      }
+    store_row<T>(p.dx, t, row, p.h, l);
+    if (p.gate) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[c][i] = f[c][i];
+      if (POST) affine<T>(y, p.post_gain, p.post_shift, l);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (COLUMNS) dgate[c][i] = fmaf(d[c][i], y[c][i], dgate[c][i]);
+          y[c][i] *= d[c][i];
+          d[c][i] *= g[c][i];
+        }
+      if (!COLUMNS) store_row<T>(p.dgate, y, row, p.h, l);
+    }
+    if (POST) {
+      float w[C][8], m[2] = {0.f, 0.f};
+      load_row<T>(w, p.post_gain, 0, 0, l);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dpost_gain[c][i] = fmaf(d[c][i], f[c][i], dpost_gain[c][i]);
+          if (LAYER) dpost_shift[c][i] += d[c][i];
+          d[c][i] *= w[c][i];
+          if (LAYER) m[0] += d[c][i];
+          m[1] = fmaf(d[c][i], f[c][i], m[1]);
+        }
+      sums(m);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[c][i] = rf * (d[c][i] - m[0] * over_h - f[c][i] * (m[1] * over_h));
+    }
+    store_row<T>(p.df, d, row, p.h, l);
+  }
+  if (!p.partials) return;
+  // [blocks][the sums that there are][h]
+  float* to = p.partials;
+  const int64_t stride = (int64_t)((p.dn ? 1 : 0) + (p.dn && LAYER && p.pre_shift ? 1 : 0) + (POST ? 1 : 0) +
+                                   (POST && LAYER && p.post_shift ? 1 : 0) + (COLUMNS ? 1 : 0)) * p.h;
+  to += blockIdx.x * stride;
+  auto leave = [&](const float (&v)[C][8]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) store_eight(to + l.col[c], v[c], l.held[c], l.held[c] >= 8 && p.h % 4 == 0);
+    to += p.h;
+  };
+  if (p.dn) leave(dpre_gain);
+  if (p.dn && LAYER && p.pre_shift) leave(dpre_shift);
+  if (POST) leave(dpost_gain);
+  if (POST && LAYER && p.post_shift) leave(dpost_shift);
+  if (COLUMNS) leave(dgate);
+}
+
+// += the blocks' partial sums [blocks][n_sums h]: a block 32 columns, a thread every eighth block's value of one, eight loads under way.
+__global__ __launch_bounds__(256) void norm_join_sum_kernel(const float* __restrict__ partials, int blocks, int h, int n_sums, SumTargets targets) {
+  __shared__ float part[8][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t width = (int64_t)n_sums * h, e = (int64_t)blockIdx.x * 32 + x;
+  float v = 0.f;
+  if (e < width) {
+    for (int b = y; b < blocks; b += 64) {
+      float u[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] = b + 8 * k < blocks ? partials[(b + 8 * k) * width + e] : 0.f;
+      v += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
+    }
+  }
+  part[y][x] = v;
+  __syncthreads();
+  if (y || e >= width) return;
+  v = ((part[0][x] + part[1][x]) + (part[2][x] + part[3][x])) + ((part[4][x] + part[5][x]) + (part[6][x] + part[7][x]));
+  const int which = (int)(e / h);
+  float* to = targets.to[0];
+#pragma unroll
+  for (int k = 1; k < kSums; ++k)
+    if (which == k) to = targets.to[k];
+  to[e - (int64_t)which * h] += v;
+}
+
+int chunks_of(int h) { return h > kMaxWaves * 64 * 8 ? 2 : 1; }
+int waves_of(int h) { return ceil_div((int)(saved8_cols(h) / 8), 64 * chunks_of(h)); }
+int blocks_of(int rows) { return std::min(rows, kMaxBlocks); }
+
+bool check(const char* what, int norm, int rows, int h, float skip, float branch, float eps) {
+  if ((norm != kNormLayer && norm != kNormRms) || rows < 1 || rows > kMaxRows || h < 1 || h > kMaxWidth || !(fabsf(skip) < 3e38f) ||
+      !(fabsf(branch) < 3e38f) || !(eps >= 0.f) || eps > 3e38f) {
+    set_error("%s: norm=%d rows=%d h=%d skip=%g branch=%g eps=%g (norm 0 or 1, 1 to %d rows, h 1 to %d, scales finite, eps finite and not "
+              "negative)", what, norm, rows, h, skip, branch, eps, kMaxRows, kMaxWidth);
+    return false;
+  }
+  return true;
+}
+// One tensor of a call: where it is, how long, whether it is written, which others may be the same tensor.
+struct Range {
+  const char* name;
+  const void* p;
+  uint64_t bytes;
+  int align;
+  bool written;
+  const void* may_be;
+};
+bool check_ranges(const char* what, const Range* r, int n) {
+  for (int i = 0; i < n; ++i) {
+    if ((uintptr_t)r[i].p % r[i].align != 0) {
+      set_error("%s: %s=%p is not aligned to %d bytes", what, r[i].name, r[i].p, r[i].align);
+      return false;
+    }
+    for (int j = 0; j < n; ++j) {
+      if (i == j || !r[i].written || !overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes)) continue;
+      if (!r[j].written && r[i].p == r[j].p && r[i].may_be == r[j].p) continue;
+      set_error("%s: %s is written and overlaps %s", what, r[i].name, r[j].name);
+      return false;
+    }
+  }
+  return true;
+}
+
+template <typename T>
+void launch_forward(const Join& p, hipStream_t stream) {
+  const int threads = 64 * waves_of(p.h);
+  if (chunks_of(p.h) == 1) norm_join_forward_kernel<T, 1><<<p.rows, threads, 0, stream>>>(p);
+  else norm_join_forward_kernel<T, 2><<<p.rows, threads, 0, stream>>>(p);
+}
+template <typename T, int C, bool LAYER>
+void launch_backward(const Join& p, int blocks, hipStream_t stream) {
+  const int threads = 64 * waves_of(p.h);
+  const bool columns = p.gate && !p.gate_per_value;
+  auto k = p.post_gain ? (columns ? norm_join_backward_kernel<T, C, LAYER, true, true> : norm_join_backward_kernel<T, C, LAYER, true, false>)
+                       : (columns ? norm_join_backward_kernel<T, C, LAYER, false, true> : norm_join_backward_kernel<T, C, LAYER, false, false>);
+  k<<<blocks, threads, 0, stream>>>(p);
+}
+template <typename T>
+void launch_backward(const Join& p, int blocks, hipStream_t stream) {
+  if (chunks_of(p.h) == 1) (p.layer ? launch_backward<T, 1, true> : launch_backward<T, 1, false>)(p, blocks, stream);
+  else (p.layer ? launch_backward<T, 2, true> : launch_backward<T, 2, false>)(p, blocks, stream);
+}
+
+}  // namespace
+
+bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* f, void* y, void* n, void* saved_f, void* saved_y,
+                       hipStream_t stream) {
+  const char* what = "norm_join_forward";
+  if (!check(what, a.norm, a.rows, a.h, a.skip, a.branch, a.eps)) return false;
+  if (!x || !f || !y || (a.pre_gain == nullptr) != (n == nullptr) || (!a.pre_gain && a.pre_shift) || (!a.post_gain && a.post_shift) ||
+      (a.norm == kNormRms && (a.pre_shift || a.post_shift)) || (a.gate_per_value != 0 && a.gate_per_value != 1)) {
+    set_error("%s: x=%p f=%p y=%p n=%p pre_gain=%p pre_shift=%p post_gain=%p post_shift=%p gate_per_value=%d (x, f and y given, n with "
+              "pre_gain, shifts with their gain and not with the RMS norm)", what, x, f, y, n, a.pre_gain, a.pre_shift, a.post_gain, a.post_shift,
+              a.gate_per_value);
+    return false;
+  }
+  const int size = dtype == kF32 ? 4 : 2;
+  const uint64_t one = (uint64_t)a.rows * a.h * size, row = (uint64_t)a.h * size, saved = saved8_bytes(a.rows, a.h);
+  const Range ranges[] = {{"y", y, one, size, true, x},           {"n", n, one, size, true, f},
+                          {"saved_f", saved_f, saved, 16, true, nullptr}, {"saved_y", saved_y, saved, 16, true, nullptr},
+                          {"x", x, one, size, false, nullptr},     {"f", f, one, size, false, nullptr},
+                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr}, {"pre_gain", a.pre_gain, row, size, false, nullptr},
+                          {"pre_shift", a.pre_shift, row, size, false, nullptr}, {"post_gain", a.post_gain, row, size, false, nullptr},
+                          {"post_shift", a.post_shift, row, size, false, nullptr}};
+  if (!check_ranges(what, ranges, sizeof(ranges) / sizeof(ranges[0]))) return false;
+  Join p = {};
+  p.x = x;
+  p.f = f;
+  p.gate = a.gate;
+  p.post_gain = a.post_gain;
+  p.post_shift = a.post_shift;
+  p.pre_gain = a.pre_gain;
+  p.pre_shift = a.pre_shift;
+  p.y = y;
+  p.n = n;
+  p.f_codes_out = (uint8_t*)saved_f;
+  p.y_codes_out = (uint8_t*)saved_y;
+  p.rows = a.rows;
+  p.h = a.h;
+  p.padded = (int)saved8_cols(a.h);
+  uintptr_t all = (uintptr_t)row;
+  for (const Range& r : ranges) all |= (uintptr_t)r.p;
+  p.vec = all % 16 == 0;
+  p.gate_per_value = a.gate_per_value;
+  p.layer = a.norm == kNormLayer;
+  p.skip = a.skip;
+  p.branch = a.branch;
+  p.eps = a.eps;
+  (dtype == kF32 ? launch_forward<float> : launch_forward<bf16>)(p, stream);
+  return launch_ok("norm_join_forward_kernel");
+}
+
+size_t norm_join_backward_workspace(int rows, int h) { return (size_t)blocks_of(rows) * kSums * h * sizeof(float); }
+
+bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream) {
+  const char* what = "norm_join_backward";
+  if (!check(what, a.norm, a.rows, a.h, a.skip, a.branch, a.eps)) return false;
+  const bool pre = b.dn != nullptr, post = a.post_gain != nullptr, gate = a.gate != nullptr, rms = a.norm == kNormRms;
+  if (!b.dx || !b.df || (!b.dy && !pre) || pre != (a.pre_gain != nullptr) || (pre && !b.y) || ((post || gate) && !b.f) || (b.n && !pre) ||
+      (a.gate_per_value != 0 && a.gate_per_value != 1) || (!pre && a.pre_shift) || (!post && a.post_shift) ||
+      (rms && (a.pre_shift || a.post_shift))) {
+    set_error("%s: dy=%p dn=%p y=%p f=%p dx=%p df=%p n=%p pre_gain=%p pre_shift=%p post_gain=%p post_shift=%p gate_per_value=%d (dx, df and dy or "
+              "dn given, dn and pre_gain both or none, y with dn, f with post_gain or gate, n only with dn, shifts with their gain and not with "
+              "the RMS norm)", what, b.dy, b.dn, b.y, b.f, b.dx, b.df, b.n, a.pre_gain, a.pre_shift, a.post_gain, a.post_shift, a.gate_per_value);
+    return false;
+  }
+  const bool columns = gate && !a.gate_per_value;
+  if (gate != (b.dgate != nullptr) || pre != (b.dpre_gain != nullptr) || (a.pre_shift != nullptr) != (b.dpre_shift != nullptr) ||
+      post != (b.dpost_gain != nullptr) || (a.post_shift != nullptr) != (b.dpost_shift != nullptr) || ((pre || post || columns) && !b.workspace)) {
+    set_error("%s: dgate=%p dpre_gain=%p dpre_shift=%p dpost_gain=%p dpost_shift=%p workspace=%p (a gradient for every parameter that is given and "
+              "no other, a workspace for their sums)", what, b.dgate, (void*)b.dpre_gain, (void*)b.dpre_shift, (void*)b.dpost_gain,
+              (void*)b.dpost_shift, (void*)b.workspace);
+    return false;
+  }
+  const int size = dtype == kF32 ? 4 : 2;
+  const uint64_t one = (uint64_t)a.rows * a.h * size, row = (uint64_t)a.h * size, saved = saved8_bytes(a.rows, a.h), sum = (uint64_t)a.h * 4;
+  const Range ranges[] = {{"dx", b.dx, one, size, true, b.dy},
+                          {"df", b.df, one, size, true, b.dn},
+                          {"dgate", b.dgate, columns ? sum : one, columns ? 4 : size, true, nullptr},
+                          {"dpre_gain", b.dpre_gain, sum, 4, true, nullptr},
+                          {"dpre_shift", b.dpre_shift, sum, 4, true, nullptr},
+                          {"dpost_gain", b.dpost_gain, sum, 4, true, nullptr},
+                          {"dpost_shift", b.dpost_shift, sum, 4, true, nullptr},
+                          {"n", b.n, one, size, true, nullptr},
+                          {"workspace", b.workspace, norm_join_backward_workspace(a.rows, a.h), 16, true, nullptr},
+                          {"dy", b.dy, one, size, false, nullptr},
+                          {"dn", b.dn, one, size, false, nullptr},
+                          {"y", pre ? b.y : nullptr, b.y_saved8 ? saved : one, b.y_saved8 ? 16 : size, false, nullptr},
+                          {"f", post || gate ? b.f : nullptr, b.f_saved8 ? saved : one, b.f_saved8 ? 16 : size, false, nullptr},
+                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr},
+                          {"pre_gain", a.pre_gain, row, size, false, nullptr},
+                          {"pre_shift", a.pre_shift, row, size, false, nullptr},
+                          {"post_gain", a.post_gain, row, size, false, nullptr},
+                          {"post_shift", a.post_shift, row, size, false, nullptr}};
+  if (!check_ranges(what, ranges, sizeof(ranges) / sizeof(ranges[0]))) return false;
+  Join p = {};
+  p.gate = a.gate;
+  p.post_gain = a.post_gain;
+  p.post_shift = a.post_shift;
+  p.pre_gain = a.pre_gain;
+  p.pre_shift = a.pre_shift;
+  p.dy = b.dy;
+  p.dn = b.dn;
+  if (b.y_saved8) p.y_codes = (const uint8_t*)b.y;
+  else p.y_in = b.y;
+  if (b.f_saved8) p.f_codes = (const uint8_t*)b.f;
+  else p.f = b.f;
+  p.n = b.n;
+  p.dx = b.dx;
+  p.df = b.df;
+  p.dgate = b.dgate;
+  const bool any = pre || post || columns;
+  p.partials = any ? (float*)b.workspace : nullptr;
+  p.rows = a.rows;
+  p.h = a.h;
+  p.padded = (int)saved8_cols(a.h);
+  uintptr_t all = (uintptr_t)row;
+  for (const Range& r : ranges)
+    if (r.align != 4 || size == 4) all |= (uintptr_t)r.p;
+  p.vec = all % 16 == 0;
+  p.gate_per_value = a.gate_per_value;
+  p.layer = !rms;
+  p.skip = a.skip;
+  p.branch = a.branch;
+  p.eps = a.eps;
+  const int blocks = blocks_of(a.rows);
+  (dtype == kF32 ? launch_backward<float> : launch_backward<bf16>)(p, blocks, stream);
+  if (!launch_ok("norm_join_backward_kernel")) return false;
+  if (!any) return true;
+  SumTargets targets = {};
+  int n = 0;
+  if (pre) targets.to[n++] = b.dpre_gain;
+  if (a.pre_shift) targets.to[n++] = b.dpre_shift;
+  if (post) targets.to[n++] = b.dpost_gain;
+  if (a.post_shift) targets.to[n++] = b.dpost_shift;
+  if (columns) targets.to[n++] = (float*)b.dgate;
+  norm_join_sum_kernel<<<(unsigned)ceil_div64((int64_t)n * a.h, 32), 256, 0, stream>>>((const float*)b.workspace, blocks, a.h, n, targets);
+  return launch_ok("norm_join_sum_kernel");
+}
+
+}  // namespace po

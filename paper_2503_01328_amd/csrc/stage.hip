@@ -34,6 +34,7 @@
 
 #include "../../include/pipeoffload.h"
 #include "kernels.h"
+#include "saved8.h"
 
 namespace po {
 
@@ -1969,6 +1970,64 @@ int po_op_pack(const void* const* seg_ptrs, const uint64_t* seg_bytes, int32_t n
 int po_op_unpack(void* const* seg_ptrs, const uint64_t* seg_bytes, int32_t n_seg, const void* packed, void* stream) {
   begin_launch();
   return ok(unpack_segments(seg_ptrs, seg_bytes, n_seg, packed, (hipStream_t)stream));
+}
+uint64_t po_op_saved8_bytes(int32_t rows, int32_t cols) {
+  return rows > 0 && cols > 0 && saved8_codes(rows, cols) / 8 <= kMaxSaved8Chunks ? saved8_bytes(rows, cols) : 0;
+}
+int po_op_save8(int32_t dtype, int32_t n, const void* const* x, const int32_t* rows, const int32_t* cols, const int32_t* ld,
+                void* const* saved, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(save8(dtype, n, x, rows, cols, ld, saved, (hipStream_t)stream));
+}
+int po_op_restore8(int32_t dtype, int32_t n, const void* const* saved, const int32_t* rows, const int32_t* cols, const int32_t* ld,
+                   void* const* x, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(restore8(dtype, n, saved, rows, cols, ld, x, (hipStream_t)stream));
+}
+int po_op_activation_forward(int32_t dtype, int32_t act, int32_t gated, const void* u, void* out, void* saved_u, int32_t rows, int32_t f,
+                             void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(activation_forward(dtype, act, gated, u, out, saved_u, rows, f, (hipStream_t)stream));
+}
+int po_op_activation_backward(int32_t dtype, int32_t act, int32_t gated, const void* u, int32_t u_saved8, const void* d_out, void* du,
+                              void* out, int32_t rows, int32_t f, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(activation_backward(dtype, act, gated, u, u_saved8, d_out, du, out, rows, f, (hipStream_t)stream));
+}
+int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const void* f, const void* post_gain, const void* post_shift,
+                            const void* gate, int32_t gate_per_value, float skip, float branch, const void* pre_gain, const void* pre_shift,
+                            void* y, void* n, void* saved_f, void* saved_y, int32_t rows, int32_t h, float eps, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  const NormJoin a{norm, post_gain, post_shift, gate, pre_gain, pre_shift, gate_per_value, skip, branch, rows, h, eps};
+  return ok(norm_join_forward(dtype, a, x, f, y, n, saved_f, saved_y, (hipStream_t)stream));
+}
+uint64_t po_op_norm_join_backward_workspace(int32_t rows, int32_t h) {
+  return rows > 0 && h > 0 ? norm_join_backward_workspace(rows, h) : 0;
+}
+int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const void* dn, const void* y, int32_t y_saved8, const void* f,
+                             int32_t f_saved8, const void* post_gain, const void* post_shift, const void* gate, int32_t gate_per_value,
+                             float skip, float branch, const void* pre_gain, const void* pre_shift, void* dx, void* df, void* dgate,
+                             float* dpost_gain, float* dpost_shift, float* dpre_gain, float* dpre_shift, void* n, void* workspace,
+                             int32_t rows, int32_t h, float eps, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  const NormJoin a{norm, post_gain, post_shift, gate, pre_gain, pre_shift, gate_per_value, skip, branch, rows, h, eps};
+  const NormJoinBackward b{dy, dn, y, f, y_saved8, f_saved8, dx, df, dgate, n, dpost_gain, dpost_shift, dpre_gain, dpre_shift, workspace};
+  return ok(norm_join_backward(dtype, a, b, (hipStream_t)stream));
+}
+uint64_t po_op_weight_grad_saved8_workspace(int32_t dtype, int32_t rows, int32_t k, int32_t n) {
+  return dtype == PO_F32 || dtype == PO_BF16 ? weight_grad_saved8_workspace(rows, k, n) : 0;
+}
+int po_op_weight_grad_saved8(int32_t dtype, const void* saved_x, const void* dy, int32_t ldy, float* dw, int32_t ldc, int32_t accumulate,
+                             void* workspace, int32_t rows, int32_t k, int32_t n, void* stream) {
+  begin_launch();
+  if (!dtype_ok(dtype)) return PO_E_INVAL;
+  return ok(weight_grad_saved8(dtype, saved_x, dy, ldy, dw, ldc, accumulate, workspace, rows, k, n, (hipStream_t)stream));
 }
 
 }  // extern "C"

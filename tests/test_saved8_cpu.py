@@ -1,0 +1,199 @@
+"""8-bit checkpoints, host side: sizes, what the entry points refuse, the kernels' registers; the 64-bit reference against autograd."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import saved8_reference as ref
+from paper_2503_01328_amd import binding as po
+
+ROOM = 1 << 20
+AT = ctypes.addressof((ctypes.c_char * (ROOM + 4096)).from_buffer(bytearray(ROOM + 4096)))
+AT += -AT % 256  # an aligned address that no launch is to see
+
+
+def at(k):
+    """The k-th of addresses that lie 64 KiB apart."""
+    return AT + (k << 16)
+
+
+def _refused(match, call, *args, **kw):
+    with pytest.raises(po.PipeOffloadError, match=match) as e:
+        call(*args, **kw, stream=0)
+    assert e.value.code == po.PO_E_INVAL
+
+
+# ---- sizes --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols,bytes_", [(0, 4, 0), (4, 0, 0), (-1, 8, 0), (1, 1, 48), (1, 32, 48), (1, 33, 80), (3, 32, 112), (128, 256, 33792),
+                                              (65536, 32768, 2 ** 31 + 2 ** 26), (65537, 32768, 0), (2 ** 26, 1, 2 ** 31 + 2 ** 26), (2 ** 31 - 1, 1, 0)])
+def test_bytes(rows, cols, bytes_):
+    assert po.po_op_saved8_bytes(rows, cols) == bytes_
+
+
+def test_workspaces_serve_fewer_rows():
+    for h in (1, 7, 256, 5120, 16384):
+        sizes = [po.po_op_norm_join_backward_workspace(r, h) for r in (1, 2, 100, 511, 512, 513, 5000, 1 << 20)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+    for dtype in (po.PO_F32, po.PO_BF16):
+        for k, n in ((1, 1), (64, 64), (256, 1024), (640, 256), (1000, 771), (2048, 2048), (4096, 16384)):
+            sizes = [po.po_op_weight_grad_saved8_workspace(dtype, r, k, n) for r in (1, 64, 65, 255, 256, 257, 511, 513, 1000, 1733, 2048, 4096, 9999, 16384, 10 ** 6)]
+            assert sizes == sorted(sizes), (dtype, k, n, sizes)
+    assert po.po_op_norm_join_backward_workspace(0, 8) == po.po_op_norm_join_backward_workspace(8, 0) == 0
+    assert po.po_op_weight_grad_saved8_workspace(7, 64, 64, 64) == po.po_op_weight_grad_saved8_workspace(po.PO_BF16, 0, 64, 64) == 0
+    assert po.po_op_weight_grad_saved8_workspace(po.PO_BF16, 64, (1 << 20) + 1, 64) == 0
+
+
+# ---- refusals -----------------------------------------------------------------------------------------------------
+BAD_TENSORS = [[(None, 4, 8, 8)], [(AT, 0, 8, 8)], [(AT, 4, 0, 8)], [(AT, 4, 8, 7)], [(AT + 1, 4, 8, 8)], [(AT, 65537, 32768, 32768)], []]
+
+
+@pytest.mark.parametrize("call", ["save8", "restore8"])
+@pytest.mark.parametrize("dtype", [po.PO_F32, po.PO_BF16])
+def test_save_refuses(call, dtype):
+    def run(tensors, saved):
+        _refused(call, po.po_op_save8 if call == "save8" else po.po_op_restore8, dtype, *((tensors, saved) if call == "save8" else (saved, tensors)))
+
+    for tensors in BAD_TENSORS:
+        run(tensors, [at(1)] * len(tensors))
+    run([(at(0), 4, 8, 8)] * 9, [at(1)] * 9)
+    run([(at(0), 4, 8, 8)], [None])
+    run([(at(0), 4, 8, 8)], [at(1) + 8])
+    run([(at(0), 4, 8, 8)], [at(0)])
+    run([(at(0), 4, 40, 40)], [at(0) + 48])
+    run([(at(0), 4, 8, 8), (at(2), 4, 8, 8)], [at(1), at(1) + 16] if call == "save8" else [at(1), at(3)][:1] + [at(2)])
+    run([(at(0), 4, 8, 8), (at(2), 4, 8, 8)], [at(2), at(1)])
+    if call == "restore8":  # outputs that share columns
+        run([(at(0), 4, 8, 20), (at(0) + 28, 4, 8, 20)], [at(1), at(2)])
+        run([(at(0), 4, 8, 8), (at(0), 4, 8, 8)], [at(1), at(2)])
+
+
+def test_save_refuses_unknown_types_and_lists_that_do_not_match():
+    _refused("unknown dtype", po.po_op_save8, 2, [(at(0), 4, 8, 8)], [at(1)])
+    _refused("unknown dtype", po.po_op_restore8, -1, [at(1)], [(at(0), 4, 8, 8)])
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        po.po_op_save8(po.PO_F32, [x], [], stream=0)
+    with pytest.raises(ValueError):
+        po.po_op_save8(po.PO_F32, [x.T], [at(1)], stream=0)
+    with pytest.raises(ValueError):
+        po.po_op_restore8(po.PO_F32, [at(1)], [x[:, ::2]], stream=0)
+
+
+ACT = dict(dtype=po.PO_BF16, act=0, gated=0, u=at(0), out=at(1), saved_u=at(2), rows=4, f=40)
+ACT_BACK = dict(dtype=po.PO_BF16, act=0, gated=0, u=at(0), u_saved8=1, d_out=at(1), du=at(2), out=at(3), rows=4, f=40)
+BAD_ACT = [dict(dtype=3), dict(act=2), dict(act=-1), dict(gated=2), dict(rows=0), dict(f=0), dict(rows=1 << 20, f=1 << 12), dict(u=None), dict(u=at(0) + 1),
+           dict(gated=1, rows=1 << 20, f=1 << 11)]
+
+
+@pytest.mark.parametrize("bad", BAD_ACT + [dict(out=None), dict(saved_u=at(2) + 8), dict(out=at(0) + 2), dict(saved_u=at(0)), dict(saved_u=at(1) + 16),
+                                           dict(gated=1, out=at(0))], ids=str)
+def test_activation_forward_refuses(bad):
+    _refused("dtype" if "dtype" in bad else "activation_forward", po.po_op_activation_forward, **{**ACT, **bad})
+
+
+@pytest.mark.parametrize("bad", BAD_ACT + [dict(u=at(0) + 8), dict(d_out=None), dict(du=None), dict(d_out=at(1) + 1), dict(du=at(0)), dict(out=at(0)),
+                                           dict(out=at(1)), dict(out=at(2) + 16), dict(du=at(1) + 2), dict(gated=1, du=at(1)),
+                                           dict(u_saved8=0, du=at(0))], ids=str)
+def test_activation_backward_refuses(bad):
+    _refused("dtype" if "dtype" in bad else "activation_backward", po.po_op_activation_backward, **{**ACT_BACK, **bad})
+
+
+JOIN = dict(dtype=po.PO_BF16, norm=0, x=at(0), f=at(1), post_gain=at(2), post_shift=at(3), gate=at(4), gate_per_value=0, skip=1.0, branch=1.0,
+            pre_gain=at(5), pre_shift=at(6), y=at(7), n=at(8), saved_f=at(9), saved_y=at(10), rows=4, h=40, eps=1e-5)
+BAD_JOIN = [dict(dtype=5), dict(norm=2), dict(norm=-1), dict(norm=1), dict(rows=0), dict(rows=(1 << 25) + 1), dict(h=0), dict(h=16385), dict(skip=math.nan),
+            dict(branch=math.inf), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(gate_per_value=2), dict(post_gain=None), dict(pre_gain=None)]
+
+
+@pytest.mark.parametrize("bad", BAD_JOIN + [dict(x=None), dict(f=None), dict(y=None), dict(n=None), dict(pre_gain=None, pre_shift=None), dict(x=at(0) + 1),
+                                            dict(saved_f=at(9) + 8), dict(saved_y=at(9)), dict(y=at(1)), dict(n=at(0)), dict(n=at(7)), dict(y=at(0) + 2),
+                                            dict(saved_f=at(1)), dict(y=at(4) - 64), dict(n=at(5)), dict(gate=at(4), gate_per_value=1, y=at(4))], ids=str)
+def test_join_forward_refuses(bad):
+    _refused("dtype" if "dtype" in bad else "norm_join_forward", po.po_op_norm_join_forward, **{**JOIN, **bad})
+
+
+BACK = dict(dtype=po.PO_BF16, norm=0, dy=at(0), dn=at(1), y=at(2), y_saved8=1, f=at(3), f_saved8=1, post_gain=at(4), post_shift=at(4) + 1024, gate=at(4) + 2048,
+            gate_per_value=0, skip=1.0, branch=1.0, pre_gain=at(4) + 4096, pre_shift=at(4) + 5120, dx=at(5), df=at(6), dgate=at(7), dpost_gain=at(8),
+            dpost_shift=at(9), dpre_gain=at(10), dpre_shift=at(11), n=at(12), workspace=at(13), rows=4, h=40, eps=1e-5)
+
+
+@pytest.mark.parametrize("bad", BAD_JOIN + [dict(dx=None), dict(df=None), dict(dy=None, dn=None), dict(dn=None), dict(y=None), dict(f=None), dict(dgate=None),
+                                            dict(gate=None), dict(dpre_gain=None), dict(dpre_shift=None), dict(dpost_gain=None), dict(dpost_shift=None),
+                                            dict(pre_shift=None), dict(post_shift=None), dict(workspace=None), dict(workspace=at(13) + 4),
+                                            dict(dpre_gain=at(10) + 2), dict(y=at(2) + 8), dict(f=at(3) + 8), dict(dx=at(1)), dict(df=at(0)), dict(dx=at(2)),
+                                            dict(df=at(3)), dict(dx=at(0) + 2), dict(n=at(1)), dict(n=at(5)), dict(dgate=at(8)), dict(dpre_gain=at(4)),
+                                            dict(workspace=at(6)), dict(dpre_shift=at(10) + 16), dict(y_saved8=0, dx=at(2)),
+                                            dict(norm=1, post_shift=None, dpost_shift=None)], ids=str)
+def test_join_backward_refuses(bad):
+    _refused("dtype" if "dtype" in bad else "norm_join_backward", po.po_op_norm_join_backward, **{**BACK, **bad})
+
+
+WEIGHT = dict(dtype=po.PO_BF16, saved_x=at(0), dy=at(2), ldy=24, dw=at(4), ldc=24, accumulate=0, workspace=at(6), rows=4, k=40, n=24)
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=9), dict(rows=0), dict(rows=(1 << 25) + 1), dict(k=0), dict(k=(1 << 20) + 1), dict(n=0), dict(n=25), dict(ldy=23),
+                                 dict(ldc=23), dict(k=1 << 20, n=1 << 20, ldy=1 << 20, ldc=1 << 20), dict(accumulate=2), dict(saved_x=None), dict(dy=None),
+                                 dict(dw=None), dict(saved_x=at(0) + 8), dict(dy=at(2) + 1), dict(dw=at(4) + 2), dict(dw=at(0)), dict(dw=at(2) + 32),
+                                 dict(rows=20000, workspace=None), dict(rows=2000, workspace=at(6) + 8), dict(rows=600, workspace=at(4))], ids=str)
+def test_weight_grad_refuses(bad):
+    _refused("dtype" if "dtype" in bad else "weight_grad_saved8", po.po_op_weight_grad_saved8, **{**WEIGHT, **bad})
+
+
+# ---- the reference ------------------------------------------------------------------------------------------------
+def test_reference_codes_are_e4m3():
+    """Every code's value, and rounding, against torch's own type."""
+    codes = torch.arange(256, dtype=torch.int64).to(torch.uint8)
+    want = codes.view(torch.float8_e4m3fn).double()
+    got = ref.decode(codes.view(1, -1), torch.full((1, 8), 127, dtype=torch.uint8), 256)[0]
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()])
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(64, 160, generator=g) * torch.exp2(torch.randint(-14, 3, (64, 160), generator=g).float())
+    x[:, ::32] = 448.0  # every scale is 1
+    c, s = ref.encode(x)
+    assert bool((s == 127).all()) and torch.equal(c, x.to(torch.float8_e4m3fn).view(torch.uint8))
+
+
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("gate", [None, 1, 2])
+def test_reference_gradients_are_autograds(rms, post, gate):
+    g = torch.Generator().manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    rows, h = 5, 37
+    p = dict(rms=rms, eps=1e-5, skip=0.75, branch=-1.25, gate=None if gate is None else rand(*((rows, h) if gate == 2 else (h,))),
+             post_gain=rand(h) if post else None, post_shift=rand(h) if post and not rms else None, pre_gain=rand(h), pre_shift=None if rms else rand(h))
+    x, f, dy, dn = (rand(rows, h) for _ in range(4))
+    leaves = {k: v.clone().requires_grad_() for k, v in dict(p, x=x, f=f).items() if torch.is_tensor(v)}
+
+    def norm(v, gain, shift):
+        out = torch.nn.functional.rms_norm(v, (h,), gain, 1e-5) if rms else torch.nn.functional.layer_norm(v, (h,), gain, shift, 1e-5)
+        return out
+
+    z = norm(leaves["f"], leaves["post_gain"], leaves.get("post_shift")) if post else leaves["f"]
+    y = 0.75 * leaves["x"] - 1.25 * (z * leaves["gate"] if gate else z)
+    n = norm(y, leaves["pre_gain"], leaves.get("pre_shift"))
+    forward = ref.join_forward(x, f, p, torch.float32)
+    torch.testing.assert_close(forward["y"].v, y.detach())
+    torch.testing.assert_close(forward["n"].v, n.detach())
+    ((y * dy).sum() + (n * dn).sum()).backward()
+    got = ref.join_backward(dy, dn, y.detach(), f, p, torch.float32, again=True)
+    names = dict(dx="x", df="f", dgate="gate", dpre_gain="pre_gain", dpre_shift="pre_shift", dpost_gain="post_gain", dpost_shift="post_shift")
+    for k, v in got.items():
+        torch.testing.assert_close(v.v, n.detach() if k == "n" else leaves[names[k]].grad)
+
+
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("gated", [False, True])
+def test_reference_slopes_are_autograds(silu, gated):
+    g = torch.Generator().manual_seed(2)
+    u = (3 * torch.randn(4, 50, generator=g, dtype=torch.float64)).requires_grad_()
+    f = 25 if gated else 50
+    a = u[:, :f]
+    v = torch.nn.functional.silu(a) if silu else torch.nn.functional.gelu(a, approximate="tanh")
+    v = v * u[:, f:] if gated else v
+    d = torch.randn(4, f, generator=g, dtype=torch.float64)
+    v.backward(d)
+    got = ref.activation_backward(u.detach(), d, silu, gated, torch.float32)
+    torch.testing.assert_close(got["du"].v, u.grad)
+    torch.testing.assert_close(got["out"].v, v.detach())
+    torch.testing.assert_close(ref.activation_forward(u.detach(), silu, gated, torch.float32).v, v.detach())
