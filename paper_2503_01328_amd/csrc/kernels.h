@@ -220,7 +220,7 @@ bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* 
                        hipStream_t stream);
 size_t norm_join_backward_workspace(int rows, int h);
 bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream);
-size_t weight_grad_saved8_workspace(int rows, int k, int n);
+size_t weight_grad_saved8_workspace(int dtype, int rows, int k, int n);
 bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy, float* dw, int ldc, int accumulate, void* workspace, int rows,
                         int k, int n, hipStream_t stream);
 

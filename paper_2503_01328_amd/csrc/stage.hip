@@ -2021,7 +2021,7 @@ int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const 
   return ok(norm_join_backward(dtype, a, b, (hipStream_t)stream));
 }
 uint64_t po_op_weight_grad_saved8_workspace(int32_t dtype, int32_t rows, int32_t k, int32_t n) {
-  return dtype == PO_F32 || dtype == PO_BF16 ? weight_grad_saved8_workspace(rows, k, n) : 0;
+  return dtype == PO_F32 || dtype == PO_BF16 ? weight_grad_saved8_workspace(dtype, rows, k, n) : 0;
 }
 int po_op_weight_grad_saved8(int32_t dtype, const void* saved_x, const void* dy, int32_t ldy, float* dw, int32_t ldc, int32_t accumulate,
                              void* workspace, int32_t rows, int32_t k, int32_t n, void* stream) {

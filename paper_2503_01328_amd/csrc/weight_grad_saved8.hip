@@ -9,13 +9,12 @@
 #include <algorithm>
 
 #include "gemm_tile.h"
+#include "gemm_wide_tile.h"
 #include "saved8.h"
 
 namespace po {
 
 namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 struct WeightGrad {
   const uint8_t *codes, *scales;
@@ -28,18 +27,6 @@ struct WeightGrad {
 };
 
 constexpr int kSlice = 64;
-
-// Sixteen codes of one row and scale as bf16.
-__device__ __forceinline__ void widen(u32x4 codes, unsigned byte, u32x4 (&out)[2]) {
-  const float scale = saved8_scale(byte);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, false);
-    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, true);
-    out[i / 2][2 * (i % 2)] = __builtin_bit_cast(unsigned, a);
-    out[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(unsigned, b);
-  }
-}
 
 // x as the sum of three bf16 numbers: its upper half, the upper half of what that leaves, and the rest.  What is not finite goes into the
 // first alone.
@@ -143,7 +130,7 @@ __global__ __launch_bounds__(256) void weight_grad_saved8_kernel(WeightGrad p) {
     for (int u = 0; u < PER; ++u) {
       const int q = u * 256 + tid, at = unit_at<TILE>(q / UNITS, q % UNITS);
       u32x4 w[2], planes[PLANES][2];
-      widen(codes[u], byte[u], w);
+      Saved8SliceLoader<128>::widen16(codes[u], byte[u], w);
       y[u].planes(planes);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -228,6 +215,23 @@ __global__ __launch_bounds__(256) void weight_grad_saved8_kernel(WeightGrad p) {
   }
 }
 
+// 64 WTM x 64 WTN results a block, in gemm_tile's pipeline: dY's slices straight into LDS, the checkpoint's through registers.
+template <int WTM, int WTN, int EPI>
+__global__ __launch_bounds__(256) void weight_grad_saved8_wide_kernel(WeightGrad p) {
+  extern __shared__ __align__(16) char smem[];
+  const int n_tiles = p.tiles_m * p.tiles_n, pid = blockIdx.x;
+  const int lin = n_tiles % 8 == 0 ? (pid % 8) * (n_tiles / 8) + pid / 8 : pid;
+  int tile_m, tile_n;
+  tile_of(lin, p.tiles_m, p.tiles_n, tile_m, tile_n);
+  const int first = blockIdx.y * p.split_rows, rows = min(p.rows - first, p.split_rows);
+  const int64_t at = (int64_t)first * p.padded;
+  const Saved8Operand x{p.codes + at, p.scales + (at >> 5), p.padded, rows};
+  Epilogue ep = {};
+  ep.acc_f32 = gridDim.y > 1 ? p.partials + (int64_t)blockIdx.y * p.k * p.n : p.dw;
+  ep.ldc = gridDim.y > 1 ? p.n : p.ldc;
+  gemm_tile<WTM, WTN, true, true, EPI, true>(p.k, p.n, rows, x, 0, (const bf16*)p.dy + (int64_t)first * p.ldy, p.ldy, ep, tile_m, tile_n, smem);
+}
+
 // dW (+)= the splits' partial results, in their order.
 __global__ __launch_bounds__(256) void weight_grad_sum_kernel(WeightGrad p, int splits) {
   const int64_t total = (int64_t)p.k * p.n;
@@ -259,10 +263,14 @@ constexpr int kMaxRows = 1 << 25, kMaxWidth = 1 << 20;
 constexpr int64_t kMaxTiles = 1 << 23;
 
 struct Form {
-  int tile, tiles_m, tiles_n, splits, split_rows;
+  int tile, tiles_m, tiles_n, splits, split_rows;  // tile: 64, 128, or 256: the wide kernel
 };
-Form form_of(int rows, int k, int n) {
+Form form_of(int rows, int k, int n, bool wide) {
   Form f;
+  if (wide && (int64_t)ceil_div(k, 256) * ceil_div(n, 256) >= 128) {
+    f = Form{256, ceil_div(k, 256), ceil_div(n, 256), 1, rows};
+    return f;
+  }
   f.tile = (int64_t)ceil_div(k, 128) * ceil_div(n, 128) >= 128 ? 128 : 64;
   f.tiles_m = ceil_div(k, f.tile);
   f.tiles_n = ceil_div(n, f.tile);
@@ -285,12 +293,20 @@ bool launch(const WeightGrad& p, const Form& f, hipStream_t stream) {
   weight_grad_saved8_kernel<T, TILE><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 256, BYTES, stream>>>(p);
   return launch_ok("weight_grad_saved8_kernel");
 }
+template <int EPI>
+bool launch_wide(const WeightGrad& p, const Form& f, hipStream_t stream) {
+  constexpr int BYTES = stages_of(4, 4) * (256 + 256) * 128;
+  static LdsLimit limit;
+  if (!limit.allow(weight_grad_saved8_wide_kernel<4, 4, EPI>, BYTES)) return false;
+  weight_grad_saved8_wide_kernel<4, 4, EPI><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 256, BYTES, stream>>>(p);
+  return launch_ok("weight_grad_saved8_wide_kernel");
+}
 
 }  // namespace
 
-size_t weight_grad_saved8_workspace(int rows, int k, int n) {
+size_t weight_grad_saved8_workspace(int dtype, int rows, int k, int n) {
   if (!sizes_ok(rows, k, n)) return 0;
-  const Form f = form_of(rows, k, n);
+  const Form f = form_of(rows, k, n, false);
   return f.splits > 1 ? (size_t)f.splits * k * n * sizeof(float) : 0;
 }
 
@@ -303,7 +319,7 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
               "least n, accumulate 0 or 1)", what, rows, k, n, ldy, ldc, accumulate, kMaxRows, kMaxWidth, (long long)kMaxTiles);
     return false;
   }
-  const size_t needed = weight_grad_saved8_workspace(rows, k, n);
+  const size_t needed = weight_grad_saved8_workspace(dtype, rows, k, n);
   if (!saved_x || !dy || !dw || (uintptr_t)saved_x % 16 != 0 || (uintptr_t)dy % size != 0 || (uintptr_t)dw % 4 != 0 ||
       (needed > 0 && (!workspace || (uintptr_t)workspace % 16 != 0))) {
     set_error("%s: saved_x=%p dy=%p dw=%p workspace=%p (a NULL pointer, or one not aligned: 16 bytes, workspace too, dy and dw to their type)",
@@ -316,7 +332,11 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
     set_error("%s: dw or workspace overlaps what is read or the other", what);
     return false;
   }
-  const Form f = form_of(rows, k, n);
+  const bool vec_y = (uintptr_t)dy % 16 == 0 && (rows == 1 || (int64_t)ldy * size % 16 == 0);
+  const bool vec_w = (uintptr_t)dw % 16 == 0 && (k == 1 || ldc % 4 == 0);
+  // The wide kernel: bf16, whole eights of columns on 16-byte boundaries, dy within 2 GiB.
+  const bool wide = dtype == kBF16 && vec_y && vec_w && n % 8 == 0 && ((int64_t)rows + 256) * ldy * 2 <= INT32_MAX;
+  const Form f = form_of(rows, k, n, wide);
   WeightGrad p = {};
   p.codes = (const uint8_t*)saved_x;
   p.scales = p.codes + saved8_codes(rows, k);
@@ -333,8 +353,9 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
   p.tiles_m = f.tiles_m;
   p.tiles_n = f.tiles_n;
   p.split_rows = f.split_rows;
-  p.vec_y = (uintptr_t)dy % 16 == 0 && (rows == 1 || (int64_t)ldy * size % 16 == 0);
-  p.vec_w = (uintptr_t)dw % 16 == 0 && (k == 1 || ldc % 4 == 0);
+  p.vec_y = vec_y;
+  p.vec_w = vec_w;
+  if (f.tile == 256) return accumulate ? launch_wide<kEpiAccumulate>(p, f, stream) : launch_wide<kEpiStoreF32>(p, f, stream);
   auto run = dtype == kF32 ? (f.tile == 128 ? launch<float, 128> : launch<float, 64>) : (f.tile == 128 ? launch<bf16, 128> : launch<bf16, 64>);
   if (!run(p, f, stream)) return false;
   if (f.splits == 1) return true;

@@ -437,7 +437,8 @@ def _weight_grad(dtype, saved, dy, dw, accumulate, k, rows=None, n=None, workspa
 
 
 WEIGHTS = [(1, 1, 1), (1, 40, 24), (7, 33, 5), (63, 64, 64), (64, 64, 72), (65, 100, 130), (200, 128, 128), (129, 256, 1024), (1000, 96, 771), (257, 300, 264),
-           (2000, 40, 56), (3000, 640, 256), (300, 2048, 2048), (130, 2056, 1544), (513, 1000, 4104)]
+           (2000, 40, 56), (3000, 640, 256), (300, 2048, 2048), (130, 2056, 1544), (513, 1000, 4104),
+           (1, 2100, 3800), (64, 2048, 4096), (127, 2056, 3784), (129, 2100, 3801), (192, 2305, 3592), (700, 2100, 3800)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -475,7 +476,8 @@ def test_weight_grad_of_whole_numbers_is_exact(gpu_device, dtype, rows, k, n):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,k,n,off", [(100, 64, 48, 0), (300, 200, 136, 0), (300, 200, 136, 1), (520, 2048, 1088, 0), (260, 2048, 1088, 3)])
+@pytest.mark.parametrize("rows,k,n,off", [(100, 64, 48, 0), (300, 200, 136, 0), (300, 200, 136, 1), (520, 2048, 1088, 0), (260, 2048, 1088, 3),
+                                            (150, 2100, 3800, 0), (150, 2100, 3800, 2)])
 def test_weight_grad_of_columns_of_wider_tensors(gpu_device, dtype, rows, k, n, off):
     """dy and dw with row strides, off 16 bytes too; what lies beside is neither read into the result (it is NaN) nor written."""
     dev, tdt = gpu_device, DT[dtype][1]
@@ -506,7 +508,7 @@ def test_weight_grad_workspace_kept_from_more_rows(gpu_device, dtype):
 
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, 3.3e38])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,k,n", [(100, 48, 64), (300, 2048, 1152)])
+@pytest.mark.parametrize("rows,k,n", [(100, 48, 64), (300, 2048, 1152), (90, 2100, 3800)])
 def test_weight_grad_special_values(gpu_device, dtype, rows, k, n, value):
     """One value that is not finite, or near the largest, in dy: its column alone, with the infinity that the formula has; in X: its row alone."""
     dev, tdt = gpu_device, DT[dtype][1]
