@@ -15,7 +15,7 @@ LIB = os.path.join(PKG, "libpipeoffload.so")
 RESOURCES = os.path.join(PKG, "kernel_resources.json")  # per kernel: registers, scratch bytes per lane, occupancy
 SOURCES = ["elementwise.hip", "gemm_generic.hip", "gemm_mfma.hip", "gemm_small.hip", "gemm_f32.hip", "attention_generic.hip", "attention_f32.hip", "attention_few.hip", "attention_mfma.hip",
            "packed_plan.hip", "attention_packed.hip", "attention_packed_f32.hip", "qk_norm_rotary.hip",
-           "saved8.hip", "activation.hip", "norm_join.hip", "weight_grad_saved8.hip",
+           "saved8.hip", "activation.hip", "norm_join.hip", "norm_join_backward_f32.hip", "norm_join_backward_bf16.hip", "weight_grad_saved8.hip",
            "schedule.cpp", "stage.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -14,115 +14,41 @@
 // hold their columns' sums of the parameter gradients in registers; a second launch adds the blocks' in a fixed order: no atomics.
 #include <algorithm>
 
-#include "saved8.h"
+#include "norm_join.h"
 
 namespace po {
 
+using namespace norm_join;
+
 namespace {
-
-constexpr int kMaxWaves = 16, kMaxWidth = kMaxWaves * 64 * 8 * 2, kMaxRows = 1 << 25;
-constexpr int kMaxBlocks = 512;  // of the backward: each leaves a partial sum of every parameter's gradient
-
-struct Join {
-  const void *x, *f, *gate, *post_gain, *post_shift, *pre_gain, *pre_shift;
-  const void *dy, *dn, *y_in;
-  const uint8_t *f_codes, *y_codes;  // backward: the checkpoints, where f and y_in are null
-  uint8_t *f_codes_out, *y_codes_out;
-  void *y, *n, *dx, *df, *dgate;
-  float* partials;
-  int rows, h, padded, vec, gate_per_value, layer;
-  float skip, branch, eps;
-};
-
-// Sum over a wave, the same in every lane: rows of 16 lanes by exchanges, then the four rows.
-__device__ __forceinline__ float sum_of_wave(float v) {
-#define PO_ADD_DPP(ctrl) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true))
-  PO_ADD_DPP(0xb1);   // neighbours
-  PO_ADD_DPP(0x4e);   // pairs of four
-  PO_ADD_DPP(0x141);  // half rows mirrored
-  PO_ADD_DPP(0x140);  // rows mirrored
-#undef PO_ADD_DPP
-  auto row = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
-  return (row(0) + row(16)) + (row(32) + row(48));
-}
-// Sums of N values over the block.  Two buffers in turn: who writes one has passed the barrier behind the other's reads.
-struct BlockSums {
-  float (*room)[4][kMaxWaves];
-  int turn = 0, waves;
-  template <int N>
-  __device__ __forceinline__ void operator()(float (&v)[N]) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = sum_of_wave(v[k]);
-    if (waves == 1) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float(*r)[kMaxWaves] = room[turn];
-    turn ^= 1;
-    if (lane == 0) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) r[k][wave] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      float s = 0.f;
-      for (int w = 0; w < waves; ++w) s += r[k][w];
-      v[k] = s;
-    }
-  }
-};
 
 // A lane's columns: eights waves * 64 lanes apart.  held: how many of an eight's columns there are.
 struct Lane {
-  int col[2], held[2];
-  bool whole[2], padded[2];  // all eight, 16-byte loads; a chunk of the checkpoint
+  unsigned col[4];
+  int held[4];
+  bool whole[4], padded[4];  // all eight, 16-byte loads; a chunk of the checkpoint
 };
 template <int C>
 __device__ __forceinline__ Lane lane_of(const Join& p) {
   Lane l;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    l.col[c] = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
-    l.held[c] = p.h - l.col[c];
+    l.col[c] = (c * blockDim.x + threadIdx.x) * 8;
+    l.held[c] = p.h - (int)l.col[c];
     l.whole[c] = p.vec && l.held[c] >= 8;
-    l.padded[c] = l.col[c] < p.padded;
+    l.padded[c] = (int)l.col[c] < p.padded;
   }
   return l;
-}
-template <int C>
-__device__ __forceinline__ void clear(float (&v)[C][8]) {
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
 }
 template <typename T, int C>
 __device__ __forceinline__ void load_row(float (&v)[C][8], const void* p, int64_t row, int h, const Lane& l) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) load_eight(v[c], (const T*)p + row * h + l.col[c], l.held[c], l.whole[c]);
+  for (int c = 0; c < C; ++c) load_eight(v[c], (const T*)p + row * h + l.col[c], l.held[c], l.whole[c]);  // (the row is the same in every lane)
 }
 template <typename T, int C>
 __device__ __forceinline__ void store_row(void* p, const float (&v)[C][8], int64_t row, int h, const Lane& l) {
 #pragma unroll
   for (int c = 0; c < C; ++c) store_eight((T*)p + row * h + l.col[c], v[c], l.held[c], l.whole[c]);
-}
-// A row of a checkpoint, zeros behind its last column.
-template <int C>
-__device__ __forceinline__ void load_saved(float (&v)[C][8], const uint8_t* codes, int64_t row, const Join& p, const Lane& l) {
-  const uint8_t* scales = codes + (int64_t)p.rows * p.padded;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    uint2 q = make_uint2(0, 0);
-    unsigned byte = 127;
-    if (l.held[c] > 0) {
-      const int64_t at = row * p.padded + l.col[c];
-      q = *(const uint2*)(codes + at);
-      byte = scales[at / 32];
-    }
-    saved8_decode(q, byte, v[c]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i >= l.held[c]) v[c][i] = 0.f;
-  }
 }
 template <int C>
 __device__ __forceinline__ void save_row(uint8_t* codes, const float (&v)[C][8], int64_t row, const Join& p, const Lane& l) {
@@ -200,10 +126,10 @@ __device__ __forceinline__ void affine(float (&v)[C][8], const void* gain, const
 }
 
 template <typename T, int C>
-__global__ __launch_bounds__(1024) void norm_join_forward_kernel(Join p) {
-  __shared__ float room[2][4][kMaxWaves];
+__global__ __launch_bounds__(64 * kMaxWaves) void norm_join_forward_kernel(Join p) {
+  __shared__ float room[2][2][16];
   const Lane l = lane_of<C>(p);
-  BlockSums sums{room, 0, (int)blockDim.x >> 6};
+  BlockSums sums(room);
   const int64_t row = blockIdx.x;
   float f[C][8], x[C][8], g[C][8];
   load_row<T>(f, p.f, row, p.h, l);
@@ -235,152 +161,6 @@ __global__ __launch_bounds__(1024) void norm_join_forward_kernel(Join p) {
   store_row<T>(p.n, x, row, p.h, l);
 }
 
-// Which sums a block leaves, in this order.
-enum Sum { kPreGain, kPreShift, kPostGain, kPostShift, kGate, kSums };
-struct SumTargets {
-  float* to[kSums];  // null: not among the partial sums
-};
-
-// POST: there is a norm of f; COLUMNS: a gate for each column, whose gradient is a sum.
-template <typename T, int C, bool LAYER, bool POST, bool COLUMNS>
-__global__ __launch_bounds__(1024) void norm_join_backward_kernel(Join p) {
-  __shared__ float room[2][4][kMaxWaves];
-  const Lane l = lane_of<C>(p);
-  BlockSums sums{room, 0, (int)blockDim.x >> 6};
-  const float over_h = 1.f / (float)p.h;
-  float dpre_gain[C][8], dpre_shift[C][8], dpost_gain[C][8], dpost_shift[C][8], dgate[C][8];
-  clear(dpre_gain);
-  clear(dpre_shift);
-  clear(dpost_gain);
-  clear(dpost_shift);
-  clear(dgate);
-  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-    float t[C][8], y[C][8], d[C][8], f[C][8], g[C][8];
-    if (p.dy) load_row<T>(t, p.dy, row, p.h, l);
-    else clear(t);
-    const bool uses_f = POST || p.gate;
-    if (p.dn) {
-      load_row<T>(d, p.dn, row, p.h, l);
-      if (p.y_codes) load_saved(y, p.y_codes, row, p, l);
-      else load_row<T>(y, p.y_in, row, p.h, l);
-    }
-    if (uses_f) {
-      if (p.f_codes) load_saved(f, p.f_codes, row, p, l);
-      else load_row<T>(f, p.f, row, p.h, l);
-    }
-    if (p.gate) load_row<T>(g, p.gate, p.gate_per_value ? row : 0, p.h, l);
-
-    float rf = 1.f;
-    if (p.dn || POST) {  // both norms' statistics
-      float s[2] = {0.f, 0.f};
-      if (LAYER) {
-        if (p.dn) s[0] = sum_of(y);
-        if (POST) s[1] = sum_of(f);
-        sums(s);
-        if (p.dn) centre(y, s[0] * over_h, l);
-        if (POST) centre(f, s[1] * over_h, l);
-      }
-      s[0] = p.dn ? dot_of(y, y) : 0.f;
-      s[1] = POST ? dot_of(f, f) : 0.f;
-      sums(s);
-      rf = rsqrtf(s[1] * over_h + p.eps);
-      if (POST) {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) f[c][i] *= rf;
-      }
-      if (p.dn) {
-        const float r = rsqrtf(s[0] * over_h + p.eps);
-        float w[C][8];
-        load_row<T>(w, p.pre_gain, 0, 0, l);
-        float m[2] = {0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            y[c][i] *= r;
-            dpre_gain[c][i] = fmaf(d[c][i], y[c][i], dpre_gain[c][i]);
-            if (LAYER) dpre_shift[c][i] += d[c][i];
-            d[c][i] *= w[c][i];
-            if (LAYER) m[0] += d[c][i];
-            m[1] = fmaf(d[c][i], y[c][i], m[1]);
-          }
-        sums(m);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) t[c][i] = fmaf(r, d[c][i] - m[0] * over_h - y[c][i] * (m[1] * over_h), t[c][i]);
-        if (p.n) {
-          affine<T>(y, p.pre_gain, p.pre_shift, l);
-          store_row<T>(p.n, y, row, p.h, l);
-        }
-      }
-    }
-    // what f's branch gets
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        d[c][i] = p.branch * t[c][i];
-        t[c][i] *= p.skip;
-      }
-    store_row<T>(p.dx, t, row, p.h, l);
-    if (p.gate) {
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[c][i] = f[c][i];
-      if (POST) affine<T>(y, p.post_gain, p.post_shift, l);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (COLUMNS) dgate[c][i] = fmaf(d[c][i], y[c][i], dgate[c][i]);
-          y[c][i] *= d[c][i];
-          d[c][i] *= g[c][i];
-        }
-      if (!COLUMNS) store_row<T>(p.dgate, y, row, p.h, l);
-    }
-    if (POST) {
-      float w[C][8], m[2] = {0.f, 0.f};
-      load_row<T>(w, p.post_gain, 0, 0, l);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dpost_gain[c][i] = fmaf(d[c][i], f[c][i], dpost_gain[c][i]);
-          if (LAYER) dpost_shift[c][i] += d[c][i];
-          d[c][i] *= w[c][i];
-          if (LAYER) m[0] += d[c][i];
-          m[1] = fmaf(d[c][i], f[c][i], m[1]);
-        }
-      sums(m);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[c][i] = rf * (d[c][i] - m[0] * over_h - f[c][i] * (m[1] * over_h));
-    }
-    store_row<T>(p.df, d, row, p.h, l);
-  }
-  if (!p.partials) return;
-  // [blocks][the sums that there are][h]
-  float* to = p.partials;
-  const int64_t stride = (int64_t)((p.dn ? 1 : 0) + (p.dn && LAYER && p.pre_shift ? 1 : 0) + (POST ? 1 : 0) +
-                                   (POST && LAYER && p.post_shift ? 1 : 0) + (COLUMNS ? 1 : 0)) * p.h;
-  to += blockIdx.x * stride;
-  auto leave = [&](const float (&v)[C][8]) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) store_eight(to + l.col[c], v[c], l.held[c], l.held[c] >= 8 && p.h % 4 == 0);
-    to += p.h;
-  };
-  if (p.dn) leave(dpre_gain);
-  if (p.dn && LAYER && p.pre_shift) leave(dpre_shift);
-  if (POST) leave(dpost_gain);
-  if (POST && LAYER && p.post_shift) leave(dpost_shift);
-  if (COLUMNS) leave(dgate);
-}
-
 // += the blocks' partial sums [blocks][n_sums h]: a block 32 columns, a thread every eighth block's value of one, eight loads under way.
 __global__ __launch_bounds__(256) void norm_join_sum_kernel(const float* __restrict__ partials, int blocks, int h, int n_sums, SumTargets targets) {
   __shared__ float part[8][33];
@@ -407,9 +187,7 @@ __global__ __launch_bounds__(256) void norm_join_sum_kernel(const float* __restr
   to[e - (int64_t)which * h] += v;
 }
 
-int chunks_of(int h) { return h > kMaxWaves * 64 * 8 ? 2 : 1; }
-int waves_of(int h) { return ceil_div((int)(saved8_cols(h) / 8), 64 * chunks_of(h)); }
-int blocks_of(int rows) { return std::min(rows, kMaxBlocks); }
+int forward_chunks(int h) { return h <= 64 * 8 ? 1 : h <= kMaxWaves * 64 * 8 * 2 ? 2 : 4; }
 
 bool check(const char* what, int norm, int rows, int h, float skip, float branch, float eps) {
   if ((norm != kNormLayer && norm != kNormRms) || rows < 1 || rows > kMaxRows || h < 1 || h > kMaxWidth || !(fabsf(skip) < 3e38f) ||
@@ -447,24 +225,11 @@ bool check_ranges(const char* what, const Range* r, int n) {
 
 template <typename T>
 void launch_forward(const Join& p, hipStream_t stream) {
-  const int threads = 64 * waves_of(p.h);
-  if (chunks_of(p.h) == 1) norm_join_forward_kernel<T, 1><<<p.rows, threads, 0, stream>>>(p);
-  else norm_join_forward_kernel<T, 2><<<p.rows, threads, 0, stream>>>(p);
+  const int chunks = forward_chunks(p.h), threads = 64 * waves_of(p.h, chunks);
+  if (chunks == 1) norm_join_forward_kernel<T, 1><<<p.rows, threads, 0, stream>>>(p);
+  else if (chunks == 2) norm_join_forward_kernel<T, 2><<<p.rows, threads, 0, stream>>>(p);
+  else norm_join_forward_kernel<T, 4><<<p.rows, threads, 0, stream>>>(p);
 }
-template <typename T, int C, bool LAYER>
-void launch_backward(const Join& p, int blocks, hipStream_t stream) {
-  const int threads = 64 * waves_of(p.h);
-  const bool columns = p.gate && !p.gate_per_value;
-  auto k = p.post_gain ? (columns ? norm_join_backward_kernel<T, C, LAYER, true, true> : norm_join_backward_kernel<T, C, LAYER, true, false>)
-                       : (columns ? norm_join_backward_kernel<T, C, LAYER, false, true> : norm_join_backward_kernel<T, C, LAYER, false, false>);
-  k<<<blocks, threads, 0, stream>>>(p);
-}
-template <typename T>
-void launch_backward(const Join& p, int blocks, hipStream_t stream) {
-  if (chunks_of(p.h) == 1) (p.layer ? launch_backward<T, 1, true> : launch_backward<T, 1, false>)(p, blocks, stream);
-  else (p.layer ? launch_backward<T, 2, true> : launch_backward<T, 2, false>)(p, blocks, stream);
-}
-
 }  // namespace
 
 bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* f, void* y, void* n, void* saved_f, void* saved_y,
@@ -581,14 +346,15 @@ bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b,
   uintptr_t all = (uintptr_t)row;
   for (const Range& r : ranges)
     if (r.align != 4 || size == 4) all |= (uintptr_t)r.p;
-  p.vec = all % 16 == 0;
+  p.vec = all % 16 == 0 && a.h % 8 == 0;
   p.gate_per_value = a.gate_per_value;
   p.layer = !rms;
   p.skip = a.skip;
   p.branch = a.branch;
   p.eps = a.eps;
+  p.n_sums = pre + (a.pre_shift != nullptr) + post + (a.post_shift != nullptr) + columns;
   const int blocks = blocks_of(a.rows);
-  (dtype == kF32 ? launch_backward<float> : launch_backward<bf16>)(p, blocks, stream);
+  (dtype == kF32 ? launch_backward_f32 : launch_backward_bf16)(p, stream);
   if (!launch_ok("norm_join_backward_kernel")) return false;
   if (!any) return true;
   SumTargets targets = {};
