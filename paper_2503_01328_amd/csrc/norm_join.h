@@ -1,6 +1,8 @@
 // What the kernels of norm_join.hip and norm_join_backward.h share: a call's tensors, sums over a row, which parameter sums there are.
 #pragma once
 
+#include <algorithm>
+
 #include "mfma_common.h"
 #include "saved8.h"
 
@@ -8,7 +10,6 @@ namespace po {
 namespace norm_join {
 
 constexpr int kMaxWaves = 8, kMaxWidth = kMaxWaves * 64 * 8 * 4, kMaxRows = 1 << 25;
-constexpr int kMaxBlocks = 512;  // of the backward: each leaves a partial sum of every parameter's gradient
 
 struct Join {
   const void *x, *f, *gate, *post_gain, *post_shift, *pre_gain, *pre_shift;
@@ -64,6 +65,75 @@ struct BlockSums {
   }
 };
 
+// Rows are read and written through buffers that end with them: columns behind a row and tensors that are not there read as zeros, without a
+// branch.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, int64_t at, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)p + at), 0, bytes, 0x00020000);
+}
+
+// Eight columns as they lie in memory.
+template <typename T, bool VEC>
+struct Packed {
+  u32x4 v[sizeof(T) / 2];
+  // p: the tensor; row: bytes = 0 for one that is not there
+  __device__ __forceinline__ void load(const void* p, int64_t row, int h, bool there, unsigned col) {
+    const __amdgpu_buffer_rsrc_t b = row_buffer(p, row * h * (int64_t)sizeof(T), there ? h * (int)sizeof(T) : 0);
+    const int at = (int)(col * sizeof(T));
+    if constexpr (VEC) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, at + 16 * k, 0, 0));
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __builtin_amdgcn_raw_buffer_load_b32(b, at + 4 * i, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[0][i] = (unsigned)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, at + 4 * i, 0, 0) |
+                  (unsigned)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, at + 4 * i + 2, 0, 0) << 16;
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(v[i / 4][i % 4]);
+      else x[i] = __uint_as_float(i % 2 ? v[0][i / 2] & 0xffff0000u : v[0][i / 2] << 16);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        v[i / 4][i % 4] = __float_as_uint(x[i]);
+      } else if (i % 2 == 0) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const bf16x2 pair = {(bf16)x[i], (bf16)x[i + 1]};
+        v[0][i / 2] = __builtin_bit_cast(unsigned, pair);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(void* p, int64_t row, int h, unsigned col) const {
+    const __amdgpu_buffer_rsrc_t b = row_buffer(p, row * h * (int64_t)sizeof(T), h * (int)sizeof(T));
+    const int at = (int)(col * sizeof(T));
+    typedef unsigned raw __attribute__((ext_vector_type(4)));
+    if constexpr (VEC) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw, v[k]), b, at + 16 * k, 0, 0);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) __builtin_amdgcn_raw_buffer_store_b32(v[i / 4][i % 4], b, at + 4 * i, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(v[0][i / 2] >> (16 * (i % 2))), b, at + 2 * i, 0, 0);
+    }
+  }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_chunk(void* p, const float (&x)[8], int64_t row, int h, unsigned col) {
+  Packed<T, VEC> w;
+  w.set(x);
+  w.store(p, row, h, col);
+}
+
 // Which sums a block leaves, in this order.
 enum Sum { kPreGain, kPreShift, kPostGain, kPostShift, kGate, kSums };
 struct SumTargets {
@@ -72,7 +142,12 @@ struct SumTargets {
 
 // Waves that a row of h columns takes, `chunks` eights a lane.
 inline int waves_of(int h, int chunks) { return ceil_div((int)(saved8_cols(h) / 8), 64 * chunks); }
-inline int blocks_of(int rows) { return rows < kMaxBlocks ? rows : kMaxBlocks; }
+// Blocks of the backward, each of which leaves a partial sum of every parameter's gradient: what the chip holds at once, at most 1024.
+// bf16, us with the sums, 256 / 512 / 768 blocks: 4096 rows of 4096 (four waves a row) 62 49 51, 16384 rows of 5120 (five) 221 234 241.
+inline int blocks_of(int rows, int h) {
+  const int most = std::min(1024, 256 * std::max(1, kMaxWaves / waves_of(h, h <= 64 * 8 ? 1 : 2)));
+  return rows < most ? rows : most;
+}
 
 // norm_join_backward_f32.hip, norm_join_backward_bf16.hip: dx, df, dgate, n and the blocks' partial sums.
 void launch_backward_f32(const Join& p, hipStream_t stream);

@@ -22,86 +22,28 @@ using namespace norm_join;
 
 namespace {
 
-// A lane's columns: eights waves * 64 lanes apart.  held: how many of an eight's columns there are.
-struct Lane {
-  unsigned col[4];
-  int held[4];
-  bool whole[4], padded[4];  // all eight, 16-byte loads; a chunk of the checkpoint
-};
+// v becomes N(v); held: columns of each eight that there are.
 template <int C>
-__device__ __forceinline__ Lane lane_of(const Join& p) {
-  Lane l;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    l.col[c] = (c * blockDim.x + threadIdx.x) * 8;
-    l.held[c] = p.h - (int)l.col[c];
-    l.whole[c] = p.vec && l.held[c] >= 8;
-    l.padded[c] = (int)l.col[c] < p.padded;
-  }
-  return l;
-}
-template <typename T, int C>
-__device__ __forceinline__ void load_row(float (&v)[C][8], const void* p, int64_t row, int h, const Lane& l) {
-#pragma unroll
-  for (int c = 0; c < C; ++c) load_eight(v[c], (const T*)p + row * h + l.col[c], l.held[c], l.whole[c]);  // (the row is the same in every lane)
-}
-template <typename T, int C>
-__device__ __forceinline__ void store_row(void* p, const float (&v)[C][8], int64_t row, int h, const Lane& l) {
-#pragma unroll
-  for (int c = 0; c < C; ++c) store_eight((T*)p + row * h + l.col[c], v[c], l.held[c], l.whole[c]);
-}
-template <int C>
-__device__ __forceinline__ void save_row(uint8_t* codes, const float (&v)[C][8], int64_t row, const Join& p, const Lane& l) {
-  uint8_t* scales = codes + (int64_t)p.rows * p.padded;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    unsigned byte;
-    const uint2 q = saved8_encode(v[c], byte);
-    if (l.padded[c]) {
-      const int64_t at = row * p.padded + l.col[c];
-      *(uint2*)(codes + at) = q;
-      if (threadIdx.x % 4 == 0) scales[at / 32] = (uint8_t)byte;
-    }
-  }
-}
-template <int C>
-__device__ __forceinline__ float sum_of(const float (&v)[C][8]) {
-  float s = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += v[c][i];
-  return s;
-}
-template <int C>
-__device__ __forceinline__ float dot_of(const float (&v)[C][8], const float (&w)[C][8]) {
-  float s = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(v[c][i], w[c][i], s);
-  return s;
-}
-// v - mean where there is a column, zero elsewhere.
-template <int C>
-__device__ __forceinline__ void centre(float (&v)[C][8], float mean, const Lane& l) {
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = i < l.held[c] ? v[c][i] - mean : 0.f;
-}
-
-// v becomes N(v).
-template <int C>
-__device__ __forceinline__ void normalise(float (&v)[C][8], const Join& p, const Lane& l, BlockSums& sums) {
-  float s[1];
+__device__ __forceinline__ void normalise(float (&v)[C][8], const int (&held)[C], const Join& p, BlockSums& sums) {
+  float s[1] = {0.f};
   const float over_h = 1.f / (float)p.h;
   if (p.layer) {
-    s[0] = sum_of(v);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[0] += v[c][i];
     sums(s);
-    centre(v, s[0] * over_h, l);
+    const float mean = s[0] * over_h;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = i < held[c] ? v[c][i] - mean : 0.f;
+    s[0] = 0.f;
   }
-  s[0] = dot_of(v, v);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[0] = fmaf(v[c][i], v[c][i], s[0]);
   sums(s);
   const float r = rsqrtf(s[0] * over_h + p.eps);
 #pragma unroll
@@ -109,82 +51,111 @@ __device__ __forceinline__ void normalise(float (&v)[C][8], const Join& p, const
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[c][i] *= r;
 }
-template <typename T, int C>
-__device__ __forceinline__ void affine(float (&v)[C][8], const void* gain, const void* shift, const Lane& l) {
-  float w[C][8];
-  load_row<T>(w, gain, 0, 0, l);
+template <typename P, int C>
+__device__ __forceinline__ void affine(float (&v)[C][8], const P (&gain)[C], const P (&shift)[C]) {
+  float g[8], a[8];
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+  for (int c = 0; c < C; ++c) {
+    gain[c].get(g);
+    shift[c].get(a);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] *= w[c][i];
-  if (!shift) return;
-  load_row<T>(w, shift, 0, 0, l);
+    for (int i = 0; i < 8; ++i) v[c][i] = fmaf(v[c][i], g[i], a[i]);
+  }
+}
+template <int C>
+__device__ __forceinline__ void save_row(uint8_t* codes, const float (&v)[C][8], const unsigned (&col)[C], int64_t row, const Join& p) {
+  uint8_t* scales = codes + (int64_t)p.rows * p.padded;
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] += w[c][i];
+  for (int c = 0; c < C; ++c) {
+    unsigned byte;
+    const uint2 q = saved8_encode(v[c], byte);
+    if ((int)col[c] < p.padded) {
+      const int64_t at = row * p.padded + col[c];
+      *(uint2*)(codes + at) = q;
+      if (threadIdx.x % 4 == 0) scales[at / 32] = (uint8_t)byte;
+    }
+  }
 }
 
-template <typename T, int C>
+// VEC: rows of whole eights on 16-byte boundaries.
+template <typename T, int C, bool VEC>
 __global__ __launch_bounds__(64 * kMaxWaves) void norm_join_forward_kernel(Join p) {
   __shared__ float room[2][2][16];
-  const Lane l = lane_of<C>(p);
-  BlockSums sums(room);
   const int64_t row = blockIdx.x;
-  float f[C][8], x[C][8], g[C][8];
-  load_row<T>(f, p.f, row, p.h, l);
-  load_row<T>(x, p.x, row, p.h, l);
-  if (p.gate) load_row<T>(g, p.gate, p.gate_per_value ? row : 0, p.h, l);
-  if (p.f_codes_out) save_row(p.f_codes_out, f, row, p, l);
+  unsigned col[C];
+  int held[C];
+  Packed<T, VEC> f_in[C], x_in[C], g_in[C], post_gain[C], post_shift[C], pre_gain[C], pre_shift[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    col[c] = (c * blockDim.x + threadIdx.x) * 8;
+    held[c] = p.h - (int)col[c];
+    f_in[c].load(p.f, row, p.h, true, col[c]);
+    x_in[c].load(p.x, row, p.h, true, col[c]);
+    g_in[c].load(p.gate, p.gate_per_value ? row : 0, p.h, p.gate, col[c]);
+    post_gain[c].load(p.post_gain, 0, p.h, p.post_gain, col[c]);
+    post_shift[c].load(p.post_shift, 0, p.h, p.post_shift, col[c]);
+    pre_gain[c].load(p.pre_gain, 0, p.h, p.pre_gain, col[c]);
+    pre_shift[c].load(p.pre_shift, 0, p.h, p.pre_shift, col[c]);
+  }
+  BlockSums sums(room);
+  float f[C][8], x[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) f_in[c].get(f[c]);
+  if (p.f_codes_out) save_row(p.f_codes_out, f, col, row, p);
   if (p.post_gain) {
-    normalise(f, p, l, sums);
-    affine<T>(f, p.post_gain, p.post_shift, l);
+    normalise(f, held, p, sums);
+    affine(f, post_gain, post_shift);
   }
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+  for (int c = 0; c < C; ++c) {
+    float g[8];
+    x_in[c].get(x[c]);
+    g_in[c].get(g);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float z = p.gate ? f[c][i] * g[c][i] : f[c][i];
+      const float z = p.gate ? f[c][i] * g[i] : f[c][i];
       x[c][i] = fmaf(p.skip, x[c][i], p.branch * z);
     }
-  store_row<T>(p.y, x, row, p.h, l);
-  if (p.y_codes_out) {
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[c][i] = to_f32(from_f32<T>(x[c][i]));
-    save_row(p.y_codes_out, f, row, p, l);
+    Packed<T, VEC> stored;
+    stored.set(x[c]);
+    stored.store(p.y, row, p.h, col[c]);
+    stored.get(f[c]);  // y as it is stored
   }
+  if (p.y_codes_out) save_row(p.y_codes_out, f, col, row, p);
   if (!p.pre_gain) return;
-  normalise(x, p, l, sums);
-  affine<T>(x, p.pre_gain, p.pre_shift, l);
-  store_row<T>(p.n, x, row, p.h, l);
+  normalise(x, held, p, sums);
+  affine(x, pre_gain, pre_shift);
+#pragma unroll
+  for (int c = 0; c < C; ++c) store_chunk<T, VEC>(p.n, x[c], row, p.h, col[c]);
 }
 
-// += the blocks' partial sums [blocks][n_sums h]: a block 32 columns, a thread every eighth block's value of one, eight loads under way.
-__global__ __launch_bounds__(256) void norm_join_sum_kernel(const float* __restrict__ partials, int blocks, int h, int n_sums, SumTargets targets) {
-  __shared__ float part[8][33];
+// += the blocks' partial sums [blocks][n_sums h]: a block 32 columns, a thread every 32nd block's value of one, eight loads under way.
+__global__ __launch_bounds__(1024) void norm_join_sum_kernel(const float* __restrict__ partials, int blocks, int h, int n_sums, SumTargets targets) {
+  __shared__ float part[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int64_t width = (int64_t)n_sums * h, e = (int64_t)blockIdx.x * 32 + x;
   float v = 0.f;
   if (e < width) {
-    for (int b = y; b < blocks; b += 64) {
+    for (int b = y; b < blocks; b += 256) {
       float u[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) u[k] = b + 8 * k < blocks ? partials[(b + 8 * k) * width + e] : 0.f;
+      for (int k = 0; k < 8; ++k) u[k] = b + 32 * k < blocks ? partials[(b + 32 * k) * width + e] : 0.f;
       v += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
     }
   }
   part[y][x] = v;
-  __syncthreads();
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    __syncthreads();
+    if (y < o) part[y][x] += part[y + o][x];
+  }
   if (y || e >= width) return;
-  v = ((part[0][x] + part[1][x]) + (part[2][x] + part[3][x])) + ((part[4][x] + part[5][x]) + (part[6][x] + part[7][x]));
   const int which = (int)(e / h);
   float* to = targets.to[0];
 #pragma unroll
   for (int k = 1; k < kSums; ++k)
     if (which == k) to = targets.to[k];
-  to[e - (int64_t)which * h] += v;
+  to[e - (int64_t)which * h] += part[0][x];
 }
 
 int forward_chunks(int h) { return h <= 64 * 8 ? 1 : h <= kMaxWaves * 64 * 8 * 2 ? 2 : 4; }
@@ -223,13 +194,14 @@ bool check_ranges(const char* what, const Range* r, int n) {
   return true;
 }
 
-template <typename T>
+template <typename T, bool VEC>
 void launch_forward(const Join& p, hipStream_t stream) {
   const int chunks = forward_chunks(p.h), threads = 64 * waves_of(p.h, chunks);
-  if (chunks == 1) norm_join_forward_kernel<T, 1><<<p.rows, threads, 0, stream>>>(p);
-  else if (chunks == 2) norm_join_forward_kernel<T, 2><<<p.rows, threads, 0, stream>>>(p);
-  else norm_join_forward_kernel<T, 4><<<p.rows, threads, 0, stream>>>(p);
+  if (chunks == 1) norm_join_forward_kernel<T, 1, VEC><<<p.rows, threads, 0, stream>>>(p);
+  else if (chunks == 2) norm_join_forward_kernel<T, 2, VEC><<<p.rows, threads, 0, stream>>>(p);
+  else norm_join_forward_kernel<T, 4, VEC><<<p.rows, threads, 0, stream>>>(p);
 }
+
 }  // namespace
 
 bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* f, void* y, void* n, void* saved_f, void* saved_y,
@@ -269,17 +241,18 @@ bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* 
   p.padded = (int)saved8_cols(a.h);
   uintptr_t all = (uintptr_t)row;
   for (const Range& r : ranges) all |= (uintptr_t)r.p;
-  p.vec = all % 16 == 0;
+  p.vec = all % 16 == 0 && a.h % 8 == 0;
   p.gate_per_value = a.gate_per_value;
   p.layer = a.norm == kNormLayer;
   p.skip = a.skip;
   p.branch = a.branch;
   p.eps = a.eps;
-  (dtype == kF32 ? launch_forward<float> : launch_forward<bf16>)(p, stream);
+  (dtype == kF32 ? (p.vec ? launch_forward<float, true> : launch_forward<float, false>)
+                 : (p.vec ? launch_forward<bf16, true> : launch_forward<bf16, false>))(p, stream);
   return launch_ok("norm_join_forward_kernel");
 }
 
-size_t norm_join_backward_workspace(int rows, int h) { return (size_t)blocks_of(rows) * kSums * h * sizeof(float); }
+size_t norm_join_backward_workspace(int rows, int h) { return (size_t)blocks_of(rows, h) * kSums * h * sizeof(float); }
 
 bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream) {
   const char* what = "norm_join_backward";
@@ -353,7 +326,7 @@ bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b,
   p.branch = a.branch;
   p.eps = a.eps;
   p.n_sums = pre + (a.pre_shift != nullptr) + post + (a.post_shift != nullptr) + columns;
-  const int blocks = blocks_of(a.rows);
+  const int blocks = blocks_of(a.rows, a.h);
   (dtype == kF32 ? launch_backward_f32 : launch_backward_bf16)(p, stream);
   if (!launch_ok("norm_join_backward_kernel")) return false;
   if (!any) return true;
@@ -364,7 +337,7 @@ bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b,
   if (post) targets.to[n++] = b.dpost_gain;
   if (a.post_shift) targets.to[n++] = b.dpost_shift;
   if (columns) targets.to[n++] = (float*)b.dgate;
-  norm_join_sum_kernel<<<(unsigned)ceil_div64((int64_t)n * a.h, 32), 256, 0, stream>>>((const float*)b.workspace, blocks, a.h, n, targets);
+  norm_join_sum_kernel<<<(unsigned)ceil_div64((int64_t)n * a.h, 32), 1024, 0, stream>>>((const float*)b.workspace, blocks, a.h, n, targets);
   return launch_ok("norm_join_sum_kernel");
 }
 

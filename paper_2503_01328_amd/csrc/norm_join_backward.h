@@ -15,73 +15,6 @@ namespace norm_join {
 // time.
 enum Form { kFromSaved, kFromTensors, kAny };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, int64_t at, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)p + at), 0, bytes, 0x00020000);
-}
-
-// Eight columns as they lie in memory.
-template <typename T, bool VEC>
-struct Packed {
-  u32x4 v[sizeof(T) / 2];
-  // p: the tensor; row: bytes = 0 for one that is not there
-  __device__ __forceinline__ void load(const void* p, int64_t row, int h, bool there, unsigned col) {
-    const __amdgpu_buffer_rsrc_t b = row_buffer(p, row * h * (int64_t)sizeof(T), there ? h * (int)sizeof(T) : 0);
-    const int at = (int)(col * sizeof(T));
-    if constexpr (VEC) {
-#pragma unroll
-      for (int k = 0; k < (int)sizeof(T) / 2; ++k) v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, at + 16 * k, 0, 0));
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __builtin_amdgcn_raw_buffer_load_b32(b, at + 4 * i, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        v[0][i] = (unsigned)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, at + 4 * i, 0, 0) |
-                  (unsigned)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, at + 4 * i + 2, 0, 0) << 16;
-    }
-  }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(v[i / 4][i % 4]);
-      else x[i] = __uint_as_float(i % 2 ? v[0][i / 2] & 0xffff0000u : v[0][i / 2] << 16);
-    }
-  }
-  __device__ __forceinline__ void set(const float (&x)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        v[i / 4][i % 4] = __float_as_uint(x[i]);
-      } else if (i % 2 == 0) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        const bf16x2 pair = {(bf16)x[i], (bf16)x[i + 1]};
-        v[0][i / 2] = __builtin_bit_cast(unsigned, pair);
-      }
-    }
-  }
-  __device__ __forceinline__ void store(void* p, int64_t row, int h, unsigned col) const {
-    const __amdgpu_buffer_rsrc_t b = row_buffer(p, row * h * (int64_t)sizeof(T), h * (int)sizeof(T));
-    const int at = (int)(col * sizeof(T));
-    typedef unsigned raw __attribute__((ext_vector_type(4)));
-    if constexpr (VEC) {
-#pragma unroll
-      for (int k = 0; k < (int)sizeof(T) / 2; ++k) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw, v[k]), b, at + 16 * k, 0, 0);
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) __builtin_amdgcn_raw_buffer_store_b32(v[i / 4][i % 4], b, at + 4 * i, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(v[0][i / 2] >> (16 * (i % 2))), b, at + 2 * i, 0, 0);
-    }
-  }
-};
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_chunk(void* p, const float (&x)[8], int64_t row, int h, unsigned col) {
-  Packed<T, VEC> w;
-  w.set(x);
-  w.store(p, row, h, col);
-}
-
 // Eight columns of y or f.
 template <typename T, Form FORM>
 struct Source {
@@ -310,7 +243,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void norm_join_backward_kernel(Join
 template <typename T, int C, Form FORM, bool LAYER, bool POST>
 void launch_all(const Join& p, hipStream_t stream) {
   constexpr int NORMS = kSumPre | (POST ? kSumPost : 0);
-  const int blocks = blocks_of(p.rows), threads = 64 * waves_of(p.h, C);
+  const int blocks = blocks_of(p.rows, p.h), threads = 64 * waves_of(p.h, C);
   if (p.gate && !p.gate_per_value) norm_join_backward_kernel<T, C, FORM, LAYER, POST, NORMS | kSumGate, true><<<blocks, threads, 0, stream>>>(p);
   else norm_join_backward_kernel<T, C, FORM, LAYER, POST, NORMS, true><<<blocks, threads, 0, stream>>>(p);
 }
@@ -321,7 +254,7 @@ void launch_form(const Join& p, hipStream_t stream) {
 }
 template <typename T>
 void launch_any(const Join& p, hipStream_t stream) {
-  const int blocks = blocks_of(p.rows);
+  const int blocks = blocks_of(p.rows, p.h);
   if (p.h <= kMaxWaves * 64 * 8) {
     norm_join_backward_kernel<T, 1, kAny, true, true, kSumPre | kSumPost | kSumGate, true><<<blocks, 64 * waves_of(p.h, 1), 0, stream>>>(p);
     return;

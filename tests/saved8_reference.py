@@ -165,7 +165,7 @@ def join_forward(x, f, p, dtype):
 
 def join_backward(dy, dn, y, f, p, dtype, again=False):
     rms, eps, rows = p["rms"], p["eps"], f.shape[0] if f is not None else (dy if dy is not None else dn).shape[0]
-    depth = rows / 512 + 40  # a block's rows one after another (at most 512 blocks), then the blocks'
+    depth = rows / 256 + 40  # a block's rows one after another (256 blocks at least where there are as many rows), then the blocks'
     zero = torch.zeros_like(dy if dy is not None else dn)
     t, out = Near(dy if dy is not None else zero), {}
     if dn is not None:
