@@ -76,13 +76,13 @@ __global__ __launch_bounds__(256) void activation_forward_kernel(Act p) {
       const uint2 codes = saved8_encode(a[k], byte);
       const size_t at = (size_t)row[k] * p.padded + col[k];
       if (there) {
-        *(uint2*)(p.codes_out + at) = codes;
+        store_past(p.codes_out + at, codes);
         if (i % 4 == 0) p.scales_out[at / 32] = (uint8_t)byte;
       }
       if (GATED) {
         const uint2 more = saved8_encode(b[k], byte);
         if (there) {
-          *(uint2*)(p.codes_out + at + b_at) = more;
+          store_past(p.codes_out + at + b_at, more);
           if (i % 4 == 0) p.scales_out[(at + b_at) / 32] = (uint8_t)byte;
         }
       }

@@ -71,6 +71,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, int6
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)p + at), 0, bytes, 0x00020000);
 }
 
+constexpr int kStorePast = 2;  // a buffer store's non-temporal bit
+
 // Eight columns as they lie in memory.
 template <typename T, bool VEC>
 struct Packed {
@@ -117,7 +119,7 @@ struct Packed {
     typedef unsigned raw __attribute__((ext_vector_type(4)));
     if constexpr (VEC) {
 #pragma unroll
-      for (int k = 0; k < (int)sizeof(T) / 2; ++k) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw, v[k]), b, at + 16 * k, 0, 0);
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw, v[k]), b, at + 16 * k, 0, kStorePast);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) __builtin_amdgcn_raw_buffer_store_b32(v[i / 4][i % 4], b, at + 4 * i, 0, 0);

@@ -71,7 +71,7 @@ __device__ __forceinline__ void save_row(uint8_t* codes, const float (&v)[C][8],
     const uint2 q = saved8_encode(v[c], byte);
     if ((int)col[c] < p.padded) {
       const int64_t at = row * p.padded + col[c];
-      *(uint2*)(codes + at) = q;
+      store_past(codes + at, q);
       if (threadIdx.x % 4 == 0) scales[at / 32] = (uint8_t)byte;
     }
   }

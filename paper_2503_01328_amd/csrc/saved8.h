@@ -92,6 +92,16 @@ __device__ __forceinline__ void load_eight(float (&v)[8], const T* p, int n, boo
     for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
   }
 }
+// Results that no later part of the same kernel reads are stored past the caches (non-temporal): they are too large to be kept there, and lines
+// that are only written cost reads of others.
+__device__ __forceinline__ void store_past(void* p, uint4 v) {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u4{v.x, v.y, v.z, v.w}, reinterpret_cast<u4*>(p));
+}
+__device__ __forceinline__ void store_past(void* p, uint2 v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  __builtin_nontemporal_store(u2{v.x, v.y}, reinterpret_cast<u2*>(p));
+}
 template <typename T>
 __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int n, bool whole) {
   constexpr int V = Vec16<T>::N;
@@ -101,7 +111,7 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int n, bo
       Vec16<T> x;
 #pragma unroll
       for (int i = 0; i < V; ++i) x.v[i] = from_f32<T>(v[k + i]);
-      store16(p + k, x);
+      store_past(p + k, *reinterpret_cast<const uint4*>(&x));
     }
   } else {
 #pragma unroll

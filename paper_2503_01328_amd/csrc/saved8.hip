@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void saved8_kernel(Table8 tab) {
     if (SAVE) {
       codes[u] = saved8_encode(v[u], byte[u]);
       if (i < t.chunks) {
-        *(uint2*)(t.codes + (size_t)i * 8) = codes[u];
+        store_past(t.codes + (size_t)i * 8, codes[u]);
         if (i % 4 == 0) t.scales[i / 4] = (uint8_t)byte[u];
       }
     } else if (i < t.chunks) {
@@ -120,8 +120,8 @@ bool table_of(const char* what, bool save, int dtype, int n, const void* const* 
         return false;
       }
     }
-  // Four chunks a thread keep more loads under way; a small set spreads over more blocks instead.
-  unroll = total >= 4u * 256 * 1024 ? 4 : 1;
+  // Two chunks a thread keep more loads under way; a small set spreads over more blocks instead.
+  unroll = total >= 2u * 256 * 1024 ? 2 : 1;
   tab.n = n;
   uint64_t block = 0;
   for (int i = 0; i < n; ++i) {
@@ -146,8 +146,8 @@ template <typename T, bool SAVE>
 void launch(const Table8& tab, int unroll, hipStream_t stream) {
   const Tensor8& last = tab.t[tab.n - 1];
   const unsigned blocks = last.first_block + (unsigned)ceil_div64(last.chunks, 256 * unroll);
-  if (unroll == 4)
-    saved8_kernel<T, SAVE, 4><<<blocks, 256, 0, stream>>>(tab);
+  if (unroll == 2)
+    saved8_kernel<T, SAVE, 2><<<blocks, 256, 0, stream>>>(tab);
   else
     saved8_kernel<T, SAVE, 1><<<blocks, 256, 0, stream>>>(tab);
 }
