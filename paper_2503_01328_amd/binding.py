@@ -424,34 +424,40 @@ def po_op_saved8_bytes(rows, cols) -> int:
     return lib.po_op_saved8_bytes(rows, cols)
 
 
-def _matrices(tensors):
-    """[(pointer, rows, cols, row stride)] of 2-d tensors with neighbouring columns, or of such tuples, as C arrays."""
+# Array types by length: making one anew takes longer than filling it.
+_I32 = [C.c_int32 * n for n in range(9)]
+_VOIDP = [C.c_void_p * n for n in range(9)]
+
+
+def _matrices(tensors, saved):
+    """(n, pointers, rows, cols, row strides, checkpoints) of 2-d tensors with neighbouring columns, or of tuples of the first four, as C arrays."""
+    n = len(tensors)
+    if len(saved) != n:
+        raise ValueError("a checkpoint for every tensor is needed")
     given = []
     for t in tensors:
-        if not isinstance(t, tuple):
+        if type(t) is not tuple:
             rows, cols = t.shape
-            if cols > 1 and t.stride(1) != 1:
+            ld, inner = t.stride()
+            if inner != 1 and cols > 1:
                 raise ValueError("the columns of a row have to be neighbours")
-            t = (t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols)
+            t = (t.data_ptr(), rows, cols, ld if rows > 1 else cols)
         given.append(t)
-    n = len(given)
-    return n, (C.c_void_p * n)(*[g[0] for g in given]), *((C.c_int32 * n)(*[g[k] for g in given]) for k in (1, 2, 3))
+    ints, pointers = (_I32[n], _VOIDP[n]) if n <= 8 else (C.c_int32 * n, C.c_void_p * n)
+    x, rows, cols, ld = zip(*given) if given else ((),) * 4
+    return n, pointers(*x), ints(*rows), ints(*cols), ints(*ld), pointers(*[_ptr(s) for s in saved])
 
 
 def po_op_save8(dtype, tensors, saved, stream=None):
     """tensors: list of 2-d tensors (rows may have a stride) or (pointer, rows, cols, row stride); saved: their checkpoints' buffers."""
-    n, x, rows, cols, ld = _matrices(tensors)
-    if len(saved) != n:
-        raise ValueError("a checkpoint for every tensor is needed")
-    _check(lib.po_op_save8(dtype, n, x, rows, cols, ld, (C.c_void_p * n)(*[_ptr(s) for s in saved]), _stream(stream)))
+    n, x, rows, cols, ld, to = _matrices(tensors, saved)
+    _check(lib.po_op_save8(dtype, n, x, rows, cols, ld, to, _stream(stream)))
 
 
 def po_op_restore8(dtype, saved, tensors, stream=None):
     """saved, tensors: as for po_op_save8."""
-    n, x, rows, cols, ld = _matrices(tensors)
-    if len(saved) != n:
-        raise ValueError("a checkpoint for every tensor is needed")
-    _check(lib.po_op_restore8(dtype, n, (C.c_void_p * n)(*[_ptr(s) for s in saved]), rows, cols, ld, x, _stream(stream)))
+    n, x, rows, cols, ld, at = _matrices(tensors, saved)
+    _check(lib.po_op_restore8(dtype, n, at, rows, cols, ld, x, _stream(stream)))
 
 
 def po_op_activation_forward(dtype, act, gated, u, out, saved_u, rows, f, stream=None):

@@ -135,6 +135,14 @@ struct SliceLoader {
 // go through registers: sixteen columns of a k (one unit, one scale) at a time, loaded a whole slice before they are converted.  Four units of a
 // thread are 32 conversions and eight LDS writes a slice, beside 64 MFMAs of a wave; converting fragments instead, where a lane's eight k
 // have eight scales, would take ten times as many.
+// Eight codes with one scale as bf16, exactly.
+__device__ __forceinline__ u32x4 widen8(uint2 codes, unsigned byte) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float scale = __uint_as_float(byte << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.x, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, scale, true);
+  return u32x4{__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, c), __builtin_bit_cast(unsigned, d)};
+}
 struct Saved8Operand {
   const uint8_t *codes, *scales;
   int padded, rows;  // codes in a row; rows (K)
@@ -168,8 +176,8 @@ struct Saved8SliceLoader {
   // results that are not stored.
   __device__ __forceinline__ void load(int u) {
     const unsigned bytes = (unsigned)min(max(left, (int64_t)0), (int64_t)0xffffffe0);
-    codes[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(resource(slice, bytes), (int)at[u], 0, 0));
-    byte[u] = __builtin_amdgcn_raw_buffer_load_b8(resource(scale_slice, bytes >> 5), (int)scale_at[u], 0, 0);
+    codes[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_resource(slice, bytes), (int)at[u], 0, 0));
+    byte[u] = __builtin_amdgcn_raw_buffer_load_b8(buffer_resource(scale_slice, bytes >> 5), (int)scale_at[u], 0, 0);
   }
   __device__ __forceinline__ void advance() {
     slice += step;
@@ -177,25 +185,8 @@ struct Saved8SliceLoader {
     left -= step;
   }
   __device__ __forceinline__ void put(int u, char* stage) const {
-    u32x4 w[2];
-    widen16(codes[u], byte[u], w);
-    *reinterpret_cast<u32x4*>(stage + lds_at[u]) = w[0];
-    *reinterpret_cast<u32x4*>(stage + lds_at[u] + 16) = w[1];
-  }
-  // Sixteen codes with one scale as bf16, exactly.
-  __device__ __forceinline__ static void widen16(u32x4 codes, unsigned byte, u32x4 (&out)[2]) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const float scale = __uint_as_float(byte << 23);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, false);
-      const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, true);
-      out[i / 2][2 * (i % 2)] = __builtin_bit_cast(unsigned, a);
-      out[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(unsigned, b);
-    }
-  }
-  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t resource(const uint8_t* p, unsigned bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)bytes, 0x00020000);
+    *reinterpret_cast<u32x4*>(stage + lds_at[u]) = widen8(make_uint2(codes[u][0], codes[u][1]), byte[u]);
+    *reinterpret_cast<u32x4*>(stage + lds_at[u] + 16) = widen8(make_uint2(codes[u][2], codes[u][3]), byte[u]);
   }
 };
 

@@ -32,6 +32,13 @@ __device__ __forceinline__ i32x4 buffer_of(const void* p, unsigned bytes) {
   r[3] = 0x00020000;
   return r;
 }
+// The same for loads and stores that the compiler schedules.  What it does not see to be the same in every lane it would load in a loop over the
+// lanes' values.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_resource(const void* p, unsigned bytes) {
+  const uint64_t a = (uint64_t)(size_t)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)a), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
 constexpr unsigned kOutOfBuffer = 0xfffffff0u;  // an offset no buffer reaches
 
 // One wave-wide load of 1 KiB: lane L's 16 bytes at `offset` of the buffer land in LDS at lds_base + 16 L.  Inline

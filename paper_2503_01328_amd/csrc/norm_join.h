@@ -68,7 +68,7 @@ struct BlockSums {
 // Rows are read and written through buffers that end with them: columns behind a row and tensors that are not there read as zeros, without a
 // branch.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, int64_t at, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)p + at), 0, bytes, 0x00020000);
+  return buffer_resource((const char*)p + at, (unsigned)bytes);
 }
 
 constexpr int kStorePast = 2;  // a buffer store's non-temporal bit

@@ -23,7 +23,7 @@ struct WeightGrad {
   float* partials;  // splits > 1: [splits][k][n]
   int rows, k, n, padded, ldy, ldc, accumulate;
   int tiles_m, tiles_n, split_rows;
-  int vec_y, vec_w;  // rows of dy, of dw start on 16-byte boundaries
+  int vec_w;  // rows of dw start on 16-byte boundaries
 };
 
 constexpr int kSlice = 64;
@@ -50,166 +50,205 @@ struct Planes<float> {
   static constexpr int N = 3;
 };
 
-// Sixteen columns of a row of dY in registers, and from there into their planes.
-template <typename T>
-struct Sixteen {
-  static constexpr int V = 16 * sizeof(T) / 16;  // 16-byte pieces
+// Eight columns of a row of dY in registers, and from there into their planes.  Loads go through a buffer that ends with the slice's rows; a column
+// that is not there is asked for past its end.  VEC: 16-byte pieces that are all there or not at all.
+template <typename T, bool VEC>
+struct Eight {
+  static constexpr int V = 8 * sizeof(T) / 16;  // 16-byte pieces
   u32x4 v[V];
-  __device__ __forceinline__ void load(const T* p, int held, bool vec) {
-    if (vec && held >= 16) {
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t slice, int at, int held) {  // at: bytes; held: columns that there are
+    if constexpr (VEC) {
+      constexpr int E = 16 / sizeof(T);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p) + 16 * i);
-    } else {
-      union {
-        T e[16];
-        u32x4 u[V];
-      } w;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w.e[i] = i < held ? p[i] : (T)0.f;
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = w.u[i];
-    }
-  }
-  // plane pl's 32 bytes
-  __device__ __forceinline__ void planes(u32x4 (&out)[Planes<T>::N][2]) const {
-    if constexpr (sizeof(T) == 2) {
-      out[0][0] = v[0];
-      out[0][1] = v[1];
+      for (int i = 0; i < V; ++i)
+        v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(slice, i * E < held ? at + 16 * i : (int)kOutOfBuffer, 0, 0));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        const int from = i < held ? at + i * (int)sizeof(T) : (int)kOutOfBuffer;
+        if constexpr (sizeof(T) == 4) {
+          v[i / 4][i % 4] = __builtin_amdgcn_raw_buffer_load_b32(slice, from, 0, 0);
+        } else {
+          const unsigned e = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(slice, from, 0, 0);
+          v[0][i / 2] = i % 2 ? v[0][i / 2] | e << 16 : e;
+        }
+      }
+    }
+  }
+  // plane pl's 16 bytes
+  __device__ __forceinline__ void planes(u32x4 (&out)[Planes<T>::N]) const {
+    if constexpr (sizeof(T) == 2) {
+      out[0] = v[0];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         unsigned a[3], b[3];
         three_terms(__uint_as_float(v[i / 2][2 * (i % 2)]), a);
         three_terms(__uint_as_float(v[i / 2][2 * (i % 2) + 1]), b);
 #pragma unroll
-        for (int pl = 0; pl < 3; ++pl) out[pl][i / 4][i % 4] = a[pl] | b[pl] << 16;
+        for (int pl = 0; pl < 3; ++pl) out[pl][i] = a[pl] | b[pl] << 16;
       }
     }
   }
 };
 
 template <int TILE>
-__device__ __forceinline__ int unit_at(int row, int unit) {  // byte of a unit of sixteen columns in a slice, as fragment() reads it
+__device__ __forceinline__ int eight_at(int row, int eight) {  // byte of eight columns in a slice, as fragment() reads it
   constexpr int MASK = TILE >= 128 ? 7 : TILE / 16 - 1;
-  return row * (2 * TILE) + ((unit ^ (row & MASK)) << 5);
+  return row * (2 * TILE) + (((eight >> 1) ^ (row & MASK)) << 5) + ((eight & 1) << 4);
 }
 
-// TILE x TILE results a block, four waves of TILE / 2 x TILE / 2.
-template <typename T, int TILE>
-__global__ __launch_bounds__(256) void weight_grad_saved8_kernel(WeightGrad p) {
+// TILE x TILE results a block, WAVES waves, two of them down.  AHEAD slices are on their way into registers while one is computed: a slice is
+// 512 cycles of MFMAs (TILE 128), memory a thousand and more away.
+template <typename T, int TILE, bool VEC, int AHEAD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void weight_grad_saved8_kernel(WeightGrad p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int PLANES = Planes<T>::N, UNITS = TILE / 16, PER = kSlice * UNITS / 256, WT = TILE / 64;
+  constexpr int PLANES = Planes<T>::N, EIGHTS = TILE / 8, PER = kSlice * EIGHTS / (64 * WAVES);
+  constexpr int WM = TILE / 64, WN = 2 * TILE / (32 * WAVES);  // MFMA tiles of a wave
   constexpr int X_BYTES = kSlice * TILE * 2, STAGE = X_BYTES * (1 + PLANES);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / (WAVES / 2), wn = wave % (WAVES / 2);
   int tile_m, tile_n;
   place_of_tile(tile_of_block(), p.tiles_m, p.tiles_n, tile_m, tile_n);
   const int m0 = tile_m * TILE, n0 = tile_n * TILE;
   const int first = blockIdx.y * p.split_rows, end = min(p.rows, first + p.split_rows);
 
-  u32x4 codes[PER];
-  unsigned byte[PER];
-  Sixteen<T> y[PER];
-  auto load = [&](int r0) {
+  // Neighbouring lanes take neighbouring eights: sixteen bytes each into LDS, next to each other (sixteen columns a lane, 32 bytes apart, cost 16
+  // cycles of bank conflicts a write).
+  uint2 codes[AHEAD][PER];
+  unsigned byte[AHEAD][PER];
+  Eight<T, VEC> y[AHEAD][PER];
+  int x_at[PER], y_at[PER], y_held[PER], lds_at[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int q = u * (64 * WAVES) + tid, row = q / EIGHTS, eight = q % EIGHTS, m = m0 + 8 * eight, n = n0 + 8 * eight;
+    x_at[u] = m < p.padded ? row * p.padded + m : -1;
+    y_at[u] = (row * p.ldy + n) * (int)sizeof(T);
+    y_held[u] = p.n - n;
+    lds_at[u] = eight_at<TILE>(row, eight);
+  }
+  auto load = [&](int slot, int r0) {  // rows from `end` on read as zeros
+    const int rows = max(0, min(kSlice, end - r0));
+    const int64_t at = (int64_t)r0 * p.padded;
+    const __amdgpu_buffer_rsrc_t x = buffer_resource(p.codes + at, rows * p.padded);
+    const __amdgpu_buffer_rsrc_t scale = buffer_resource(p.scales + (at >> 5), rows * p.padded >> 5);
+    const __amdgpu_buffer_rsrc_t slice =
+        buffer_resource((const uint8_t*)p.dy + (int64_t)r0 * p.ldy * (int)sizeof(T), rows * p.ldy * (int)sizeof(T));
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int q = u * 256 + tid, row = r0 + q / UNITS, unit = q % UNITS;
-      const bool there = row < end;
-      const int m = m0 + 16 * unit, n = n0 + 16 * unit;
-      codes[u] = u32x4{0, 0, 0, 0};
-      byte[u] = 127;
-      if (there && m < p.padded) {
-        const int64_t at = (int64_t)row * p.padded + m;
-        codes[u] = *reinterpret_cast<const u32x4*>(p.codes + at);
-        byte[u] = p.scales[at >> 5];
-      }
-      y[u].load((const T*)p.dy + (int64_t)row * p.ldy + n, there ? p.n - n : 0, p.vec_y);
+      const auto q = __builtin_amdgcn_raw_buffer_load_b64(x, x_at[u] >= 0 ? x_at[u] : (int)kOutOfBuffer, 0, 0);
+      codes[slot][u] = make_uint2(q[0], q[1]);
+      byte[slot][u] = __builtin_amdgcn_raw_buffer_load_b8(scale, x_at[u] >= 0 ? x_at[u] >> 5 : (int)kOutOfBuffer, 0, 0);
+      y[slot][u].load(slice, y_at[u], y_held[u]);
     }
   };
-  auto stage = [&](char* lds) {
+  auto stage = [&](int slot, int u, char* lds) {
+    u32x4 planes[PLANES];
+    y[slot][u].planes(planes);
+    *reinterpret_cast<u32x4*>(lds + lds_at[u]) = widen8(codes[slot][u], byte[slot][u]);
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int q = u * 256 + tid, at = unit_at<TILE>(q / UNITS, q % UNITS);
-      u32x4 w[2], planes[PLANES][2];
-      Saved8SliceLoader<128>::widen16(codes[u], byte[u], w);
-      y[u].planes(planes);
+    for (int pl = 0; pl < PLANES; ++pl) *reinterpret_cast<u32x4*>(lds + X_BYTES * (1 + pl) + lds_at[u]) = planes[pl];
+  };
+  bf16x8 a[2][WM], b[2][PLANES][WN];
+  auto fragments = [&](int kk, const char* lds) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        *reinterpret_cast<u32x4*>(lds + at + 16 * h) = w[h];
+    for (int w = 0; w < WM; ++w) a[kk % 2][w] = fragment<TILE, true>((const bf16*)nullptr, lds, 32 * (wm * WM + w), kk, lane);
 #pragma unroll
-        for (int pl = 0; pl < PLANES; ++pl) *reinterpret_cast<u32x4*>(lds + X_BYTES * (1 + pl) + at + 16 * h) = planes[pl][h];
-      }
-    }
+    for (int pl = 0; pl < PLANES; ++pl)
+#pragma unroll
+      for (int w = 0; w < WN; ++w)
+        b[kk % 2][pl][w] = fragment<TILE, true>((const bf16*)nullptr, lds + X_BYTES * (1 + pl), 32 * (wn * WN + w), kk, lane);
   };
 
-  f32x16 acc[WT][WT];
+  f32x16 acc[WM][WN];
 #pragma unroll
-  for (int i = 0; i < WT; ++i)
+  for (int i = 0; i < WM; ++i)
 #pragma unroll
-    for (int j = 0; j < WT; ++j)
+    for (int j = 0; j < WN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  load(first);
-  stage(smem);
+  // Slice s lies in LDS stage s % 2 while it is computed; slot s % AHEAD holds a later one on its way.
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load(i, first + i * kSlice);
+#pragma unroll
+  for (int u = 0; u < PER; ++u) stage(0, u, smem);
+  load(0, first + AHEAD * kSlice);
   int turn = 0;
-  for (int r0 = first; r0 < end; r0 += kSlice) {
-    const bool more = r0 + kSlice < end;
-    if (more) load(r0 + kSlice);
-    __syncthreads();
-    const char* lds = smem + turn * STAGE;
+  // (whole rounds of slices: a way out between them would make the compiler wait for all loads at each; behind `end` come zeros)
+  for (int r0 = first; r0 < end; r0 += AHEAD * kSlice) {
 #pragma unroll
-    for (int kk = 0; kk < kSlice / 16; ++kk) {
-      bf16x8 a[WT], b[WT];
+    for (int i = 0; i < AHEAD; ++i) {
+      const int at = r0 + i * kSlice;
+      __syncthreads();
+      const char* lds = smem + turn * STAGE;
+      turn ^= 1;
+      const int slot = (i + 1) % AHEAD;
+      fragments(0, lds);
 #pragma unroll
-      for (int i = 0; i < WT; ++i) a[i] = fragment<TILE, true>((const bf16*)nullptr, lds, wm * (TILE / 2) + 32 * i, kk, lane);
+      for (int kk = 0; kk < kSlice / 16; ++kk) {  // the next step's fragments, this step's products, a share of the next slice
+        if (kk + 1 < kSlice / 16) fragments(kk + 1, lds);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int pl = PLANES - 1; pl >= 0; --pl) {  // the smallest terms first
+        for (int pl = PLANES - 1; pl >= 0; --pl)  // the smallest terms first
 #pragma unroll
-        for (int j = 0; j < WT; ++j)
-          b[j] = fragment<TILE, true>((const bf16*)nullptr, lds + X_BYTES * (1 + pl), wn * (TILE / 2) + 32 * j, kk, lane);
+          for (int w = 0; w < WM; ++w)
 #pragma unroll
-        for (int i = 0; i < WT; ++i)
-#pragma unroll
-          for (int j = 0; j < WT; ++j) acc[i][j] = multiply(b[j], a[i], acc[i][j]);
+            for (int j = 0; j < WN; ++j) acc[w][j] = multiply(b[kk % 2][pl][j], a[kk % 2][w], acc[w][j]);
+        if (kk < PER) stage(slot, kk, smem + turn * STAGE);  // (behind the last slice zeros, which nothing reads)
+        __builtin_amdgcn_sched_barrier(0);
       }
+      load(slot, at + (1 + AHEAD) * kSlice);
     }
-    turn ^= 1;
-    if (more) stage(smem + turn * STAGE);
   }
   __syncthreads();  // the strips reuse the stages
 
   // acc[i][j][4 q + r] = dW[m][n], m = strip row lane % 32, n = 32 j + 8 q + 4 (lane / 32) + r: strips of 32 rows through LDS, so that a row of
   // results is written by neighbouring lanes.
-  constexpr int WIDE = TILE / 2, LD = WIDE + 4, LANES = WIDE / 4, STEPS = 32 * LANES / 64;
+  constexpr int WIDE = 32 * WN, LD = WIDE + 4, LANES = WIDE / 4, STEPS = 32 * LANES / 64;
   float* strip = reinterpret_cast<float*>(smem) + wave * (32 * LD);
   const bool split = gridDim.y > 1;
   float* out = split ? p.partials + (int64_t)blockIdx.y * p.k * p.n : p.dw;
   const int ld = split ? p.n : p.ldc;
   const bool vec = split ? p.n % 4 == 0 : p.vec_w, add = !split && p.accumulate;
 #pragma unroll
-  for (int i = 0; i < WT; ++i) {
+  for (int i = 0; i < WM; ++i) {
 #pragma unroll
-    for (int j = 0; j < WT; ++j)
+    for (int j = 0; j < WN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         *reinterpret_cast<f32x4*>(strip + (lane & 31) * LD + 32 * j + 8 * q + 4 * (lane >> 5)) = v;
       }
     // (a wave reads back only what it wrote itself: program order is enough, no barrier)
+    // What is added to is read first, all of it, so that its round trips are one.
+    f32x4 old[STEPS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int piece = s * 64 + lane, r = piece / LANES, c = piece % LANES * 4;
-      const int m = m0 + wm * WIDE + 32 * i + r, n = n0 + wn * WIDE + c;
-      if (m >= p.k || n >= p.n) continue;
-      const f32x4 v = *reinterpret_cast<const f32x4*>(strip + r * LD + c);
-      float* to = out + (int64_t)m * ld + n;
+      const int piece = s * 64 + lane, m = m0 + 32 * (wm * WM + i) + piece / LANES, n = n0 + wn * WIDE + piece % LANES * 4;
+      old[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (!add || m >= p.k || n >= p.n) continue;
+      const float* from = out + (int64_t)m * ld + n;
       if (vec && n + 4 <= p.n) {
-        f32x4* t = reinterpret_cast<f32x4*>(to);
-        *t = add ? *t + v : v;
+        old[s] = *reinterpret_cast<const f32x4*>(from);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (n + e < p.n) to[e] = add ? to[e] + v[e] : v[e];
+          if (n + e < p.n) old[s][e] = from[e];
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int piece = s * 64 + lane, r = piece / LANES, c = piece % LANES * 4;
+      const int m = m0 + 32 * (wm * WM + i) + r, n = n0 + wn * WIDE + c;
+      if (m >= p.k || n >= p.n) continue;
+      const f32x4 v = old[s] + *reinterpret_cast<const f32x4*>(strip + r * LD + c);
+      float* to = out + (int64_t)m * ld + n;
+      if (vec && n + 4 <= p.n) {
+        *reinterpret_cast<f32x4*>(to) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < p.n) to[e] = v[e];
       }
     }
   }
@@ -232,66 +271,97 @@ __global__ __launch_bounds__(256) void weight_grad_saved8_wide_kernel(WeightGrad
   gemm_tile<WTM, WTN, true, true, EPI, true>(p.k, p.n, rows, x, 0, (const bf16*)p.dy + (int64_t)first * p.ldy, p.ldy, ep, tile_m, tile_n, smem);
 }
 
-// dW (+)= the splits' partial results, in their order.
+// dW (+)= the splits' partial results, in a fixed order: GROUPS threads share four results, each every GROUPS-th split's, four loads under way.
+// One for up to eight splits (4096 rows, 2048 x 1024, two splits: 37 us, eight threads 41), eight for more (16384 rows, 256 x 256, 32 splits: 16.3 us, one
+// thread, a load at a time, 31).
+template <bool VEC, int GROUPS>  // VEC: the splits start on 16-byte boundaries
 __global__ __launch_bounds__(256) void weight_grad_sum_kernel(WeightGrad p, int splits) {
+  constexpr int LANES = 256 / GROUPS;
+  __shared__ f32x4 part[GROUPS][LANES];
   const int64_t total = (int64_t)p.k * p.n;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < total; i += (int64_t)gridDim.x * 1024) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool whole = total % 4 == 0;  // then every split's start is a 16-byte boundary
-    for (int k = 0; k < splits; ++k) {
-      const float* from = p.partials + k * total + i;
-      if (whole) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(from);
+  const int x = threadIdx.x % LANES, y = threadIdx.x / LANES;
+  const int64_t i = ((int64_t)blockIdx.x * LANES + x) * 4;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  auto value = [&](int k) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (k >= splits || i >= total) return v;
+    const float* from = p.partials + k * total + i;
+    if (VEC) return *reinterpret_cast<const f32x4*>(from);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += v[e];
-      } else {
+    for (int e = 0; e < 4; ++e) v[e] = i + e < total ? from[e] : 0.f;
+    return v;
+  };
+  for (int k = y; k < splits; k += 4 * GROUPS) {
+    f32x4 v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += i + e < total ? from[e] : 0.f;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (i + e < total) {
-        const int64_t m = (i + e) / p.n, n = i + e - m * p.n;
-        float* to = p.dw + m * p.ldc + n;
-        *to = p.accumulate ? *to + s[e] : s[e];
-      }
+    for (int u = 0; u < 4; ++u) v[u] = value(k + GROUPS * u);
+    sum += (v[0] + v[1]) + (v[2] + v[3]);
   }
+  if (GROUPS > 1) {
+    part[y][x] = sum;
+    __syncthreads();
+    if (y) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) sum += part[g][x];
+  }
+  if (i >= total) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (i + e < total) {
+      const int64_t m = (i + e) / p.n, n = i + e - m * p.n;
+      float* to = p.dw + m * p.ldc + n;
+      *to = p.accumulate ? *to + sum[e] : sum[e];
+    }
 }
 
-constexpr int kMaxRows = 1 << 25, kMaxWidth = 1 << 20;
+constexpr int kMaxRows = 1 << 25, kMaxWidth = 1 << 20, kMaxPitch = 1 << 22;  // a slice's offsets fit 31 bits
 constexpr int64_t kMaxTiles = 1 << 23;
 
 struct Form {
   int tile, tiles_m, tiles_n, splits, split_rows;  // tile: 64, 128, or 256: the wide kernel
 };
-Form form_of(int rows, int k, int n, bool wide) {
-  Form f;
-  if (wide && (int64_t)ceil_div(k, 256) * ceil_div(n, 256) >= 128) {
-    f = Form{256, ceil_div(k, 256), ceil_div(n, 256), 1, rows};
-    return f;
+// At most so many splits: a round of blocks (two of the small ones to a CU), four slices each at least.
+int most_splits(int rows, int64_t tiles, int tile) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * kSlice), (tile == 128 ? 256 : 512) / tiles));
+}
+// The tile and the splits that should take least: rounds of blocks, each its slices one after another, a split's partial results written and
+// read again.  Measured, us a slice of a full round: bf16 0.77 (128 x 128, 256 blocks), 0.55 (64 x 64, 512 blocks), fp32 1.9 and 1.5; the sum 3 and 8
+// bytes a partial result at 5 TB/s.  The wide kernel from 128 of its tiles on: a round of 256 takes 1.7 a slice, for four times the work.
+Form form_of(int dtype, int rows, int k, int n, bool wide) {
+  if (wide && (int64_t)ceil_div(k, 256) * ceil_div(n, 256) >= 128) return Form{256, ceil_div(k, 256), ceil_div(n, 256), 1, rows};
+  Form best = {};
+  double least = 0;
+  for (int tile = 64; tile <= 128; tile *= 2) {
+    const int64_t tiles = (int64_t)ceil_div(k, tile) * ceil_div(n, tile), round = tile == 128 ? 256 : 512;
+    const double slice = tile == 128 ? (dtype == kF32 ? 1.9 : 0.77) : (dtype == kF32 ? 1.5 : 0.55);
+    for (int splits = most_splits(rows, tiles, tile);; splits /= 2) {
+      const int each = ceil_div(ceil_div(rows, splits), kSlice);  // slices
+      const double time = (double)ceil_div64(tiles * splits, round) * (each + 4) * slice + (splits > 1 ? 3 + splits * (double)k * n * 8 / 5e6 : 0);
+      if (best.tile == 0 || time < least) {
+        least = time;
+        best = Form{tile, ceil_div(k, tile), ceil_div(n, tile), ceil_div(rows, each * kSlice), each * kSlice};
+      }
+      if (splits <= 1) break;
+    }
   }
-  f.tile = (int64_t)ceil_div(k, 128) * ceil_div(n, 128) >= 128 ? 128 : 64;
-  f.tiles_m = ceil_div(k, f.tile);
-  f.tiles_n = ceil_div(n, f.tile);
-  const int64_t tiles = (int64_t)f.tiles_m * f.tiles_n;
-  f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * kSlice), 512 / std::max<int64_t>(tiles, 1)));
-  f.split_rows = ceil_div(ceil_div(rows, f.splits), kSlice) * kSlice;
-  f.splits = ceil_div(rows, f.split_rows);
-  return f;
+  return best;
 }
 bool sizes_ok(int rows, int k, int n) {
   return rows >= 1 && rows <= kMaxRows && k >= 1 && k <= kMaxWidth && n >= 1 && n <= kMaxWidth &&
          (int64_t)ceil_div(k, 128) * ceil_div(n, 128) <= kMaxTiles;
 }
 
-template <typename T, int TILE>
+template <typename T, int TILE, bool VEC>
 bool launch(const WeightGrad& p, const Form& f, hipStream_t stream) {
-  constexpr int BYTES = 2 * kSlice * TILE * 2 * (1 + Planes<T>::N);
+  constexpr int BYTES = 2 * kSlice * TILE * 2 * (1 + Planes<T>::N), AHEAD = 2, WAVES = TILE == 128 ? 8 : 4;
   static LdsLimit limit;
-  if (!limit.allow(weight_grad_saved8_kernel<T, TILE>, BYTES)) return false;
-  weight_grad_saved8_kernel<T, TILE><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 256, BYTES, stream>>>(p);
+  if (!limit.allow(weight_grad_saved8_kernel<T, TILE, VEC, AHEAD, WAVES>, BYTES)) return false;
+  weight_grad_saved8_kernel<T, TILE, VEC, AHEAD, WAVES><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 64 * WAVES, BYTES, stream>>>(p);
   return launch_ok("weight_grad_saved8_kernel");
+}
+template <typename T>
+bool launch(const WeightGrad& p, const Form& f, bool vec, hipStream_t stream) {
+  return (f.tile == 128 ? (vec ? launch<T, 128, true> : launch<T, 128, false>) : (vec ? launch<T, 64, true> : launch<T, 64, false>))(p, f, stream);
 }
 template <int EPI>
 bool launch_wide(const WeightGrad& p, const Form& f, hipStream_t stream) {
@@ -306,17 +376,20 @@ bool launch_wide(const WeightGrad& p, const Form& f, hipStream_t stream) {
 
 size_t weight_grad_saved8_workspace(int dtype, int rows, int k, int n) {
   if (!sizes_ok(rows, k, n)) return 0;
-  const Form f = form_of(rows, k, n, false);
-  return f.splits > 1 ? (size_t)f.splits * k * n * sizeof(float) : 0;
+  // for the most splits that either tile may take, so that a workspace for more rows serves fewer
+  int most = 1;
+  for (int tile = 64; tile <= 128; tile *= 2) most = std::max(most, most_splits(rows, (int64_t)ceil_div(k, tile) * ceil_div(n, tile), tile));
+  return most > 1 ? (size_t)most * k * n * sizeof(float) : 0;
 }
 
 bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy, float* dw, int ldc, int accumulate, void* workspace, int rows,
                         int k, int n, hipStream_t stream) {
   const char* what = "weight_grad_saved8";
   const int size = dtype == kF32 ? 4 : 2;
-  if (!sizes_ok(rows, k, n) || ldy < n || ldc < n || (accumulate != 0 && accumulate != 1)) {
-    set_error("%s: rows=%d k=%d n=%d ldy=%d ldc=%d accumulate=%d (1 to %d rows, k and n 1 to %d, %lld tiles of 128 x 128, ldy and ldc at "
-              "least n, accumulate 0 or 1)", what, rows, k, n, ldy, ldc, accumulate, kMaxRows, kMaxWidth, (long long)kMaxTiles);
+  if (!sizes_ok(rows, k, n) || ldy < n || ldy > kMaxPitch || ldc < n || (accumulate != 0 && accumulate != 1)) {
+    set_error("%s: rows=%d k=%d n=%d ldy=%d ldc=%d accumulate=%d (1 to %d rows, k and n 1 to %d, at most %lld tiles of 128 x 128, ldy and "
+              "ldc at least n, ldy at most %d, accumulate 0 or 1)", what, rows, k, n, ldy, ldc, accumulate, kMaxRows, kMaxWidth,
+              (long long)kMaxTiles, kMaxPitch);
     return false;
   }
   const size_t needed = weight_grad_saved8_workspace(dtype, rows, k, n);
@@ -336,7 +409,7 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
   const bool vec_w = (uintptr_t)dw % 16 == 0 && (k == 1 || ldc % 4 == 0);
   // The wide kernel: bf16, whole eights of columns on 16-byte boundaries, dy within 2 GiB.
   const bool wide = dtype == kBF16 && vec_y && vec_w && n % 8 == 0 && ((int64_t)rows + 256) * ldy * 2 <= INT32_MAX;
-  const Form f = form_of(rows, k, n, wide);
+  const Form f = form_of(dtype, rows, k, n, wide);
   WeightGrad p = {};
   p.codes = (const uint8_t*)saved_x;
   p.scales = p.codes + saved8_codes(rows, k);
@@ -353,14 +426,15 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
   p.tiles_m = f.tiles_m;
   p.tiles_n = f.tiles_n;
   p.split_rows = f.split_rows;
-  p.vec_y = vec_y;
   p.vec_w = vec_w;
   if (f.tile == 256) return accumulate ? launch_wide<kEpiAccumulate>(p, f, stream) : launch_wide<kEpiStoreF32>(p, f, stream);
-  auto run = dtype == kF32 ? (f.tile == 128 ? launch<float, 128> : launch<float, 64>) : (f.tile == 128 ? launch<bf16, 128> : launch<bf16, 64>);
-  if (!run(p, f, stream)) return false;
+  if (!(dtype == kF32 ? launch<float> : launch<bf16>)(p, f, vec_y && n % (16 / size) == 0, stream)) return false;
   if (f.splits == 1) return true;
-  const int64_t blocks = std::min<int64_t>(ceil_div64((int64_t)k * n, 1024), 2048);
-  weight_grad_sum_kernel<<<(unsigned)blocks, 256, 0, stream>>>(p, f.splits);
+  const bool many = f.splits > 8, whole = (int64_t)k * n % 4 == 0;
+  const unsigned blocks = (unsigned)ceil_div64((int64_t)k * n, many ? 128 : 1024);
+  auto sum = many ? (whole ? weight_grad_sum_kernel<true, 8> : weight_grad_sum_kernel<false, 8>)
+                  : (whole ? weight_grad_sum_kernel<true, 1> : weight_grad_sum_kernel<false, 1>);
+  sum<<<blocks, 256, 0, stream>>>(p, f.splits);
   return launch_ok("weight_grad_sum_kernel");
 }
 

@@ -131,7 +131,7 @@ def test_join_backward_refuses(bad):
 WEIGHT = dict(dtype=po.PO_BF16, saved_x=at(0), dy=at(2), ldy=24, dw=at(4), ldc=24, accumulate=0, workspace=at(6), rows=4, k=40, n=24)
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=9), dict(rows=0), dict(rows=(1 << 25) + 1), dict(k=0), dict(k=(1 << 20) + 1), dict(n=0), dict(n=25), dict(ldy=23),
+@pytest.mark.parametrize("bad", [dict(dtype=9), dict(rows=0), dict(rows=(1 << 25) + 1), dict(k=0), dict(k=(1 << 20) + 1), dict(n=0), dict(n=25), dict(ldy=23), dict(ldy=(1 << 22) + 1),
                                  dict(ldc=23), dict(k=1 << 20, n=1 << 20, ldy=1 << 20, ldc=1 << 20), dict(accumulate=2), dict(saved_x=None), dict(dy=None),
                                  dict(dw=None), dict(saved_x=at(0) + 8), dict(dy=at(2) + 1), dict(dw=at(4) + 2), dict(dw=at(0)), dict(dw=at(2) + 32),
                                  dict(rows=20000, workspace=None), dict(rows=2000, workspace=at(6) + 8), dict(rows=600, workspace=at(4))], ids=str)
