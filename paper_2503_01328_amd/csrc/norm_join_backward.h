@@ -50,13 +50,14 @@ __device__ __forceinline__ void centre_eight(float (&v)[8], float mean, int held
   for (int i = 0; i < 8; ++i) v[i] = FORM != kAny || i < held ? v[i] - m : 0.f;
 }
 
-// The parameter sums that a launch makes: all of them where a lane has one or two eights of columns; with four their registers do not fit, so
-// that each kind has a launch of its own, of which the last writes the outputs.
+// The parameter sums that a launch makes: all of them, but for rows that take two eights a lane and more than eight waves, whose 128
+// registers a lane do not hold them all: there each kind has a launch of its own, of which the last writes the outputs.
 enum { kSumPre = 1, kSumPost = 2, kSumGate = 4 };
 
 // LAYER: not the RMS norm.  POST: there is a norm of f.  (kAny asks the arguments for both.)  SUMS: what is summed.  OUT: whether dx, df, dgate and n are written.
-template <typename T, int C, Form FORM, bool LAYER_, bool POST_, int SUMS, bool OUT>
-__global__ __launch_bounds__(64 * kMaxWaves) void norm_join_backward_kernel(Join p) {
+// WAVES: of a block at most.
+template <typename T, int C, int WAVES, Form FORM, bool LAYER_, bool POST_, int SUMS, bool OUT>
+__global__ __launch_bounds__(64 * WAVES) void norm_join_backward_kernel(Join p) {
   __shared__ float room[2][2][16];
   constexpr bool VEC = FORM != kAny, PRE_SUM = SUMS & kSumPre, POST_SUM = SUMS & kSumPost, GATE_SUM = SUMS & kSumGate;
   const bool LAYER = FORM == kAny ? p.layer : LAYER_, POST = FORM == kAny ? p.post_gain != nullptr : POST_;
@@ -244,34 +245,42 @@ template <typename T, int C, Form FORM, bool LAYER, bool POST>
 void launch_all(const Join& p, hipStream_t stream) {
   constexpr int NORMS = kSumPre | (POST ? kSumPost : 0);
   const int blocks = blocks_of(p.rows, p.h), threads = 64 * waves_of(p.h, C);
-  if (p.gate && !p.gate_per_value) norm_join_backward_kernel<T, C, FORM, LAYER, POST, NORMS | kSumGate, true><<<blocks, threads, 0, stream>>>(p);
-  else norm_join_backward_kernel<T, C, FORM, LAYER, POST, NORMS, true><<<blocks, threads, 0, stream>>>(p);
+  if (p.gate && !p.gate_per_value) norm_join_backward_kernel<T, C, 8, FORM, LAYER, POST, NORMS | kSumGate, true><<<blocks, threads, 0, stream>>>(p);
+  else norm_join_backward_kernel<T, C, 8, FORM, LAYER, POST, NORMS, true><<<blocks, threads, 0, stream>>>(p);
 }
-template <typename T, int C, Form FORM>
+// Sixteen waves: each kind of sums in a launch of its own, the outputs with the last (dx may be dy, df dn).
+template <typename T, Form FORM, bool LAYER, bool POST>
+void launch_wide(const Join& p, hipStream_t stream) {
+  const int blocks = blocks_of(p.rows, p.h), threads = 64 * waves_of(p.h, 2);
+  if (p.gate && !p.gate_per_value) norm_join_backward_kernel<T, 2, 16, FORM, LAYER, POST, kSumGate, false><<<blocks, threads, 0, stream>>>(p);
+  if (p.post_gain) norm_join_backward_kernel<T, 2, 16, FORM, LAYER, POST, kSumPost, false><<<blocks, threads, 0, stream>>>(p);
+  norm_join_backward_kernel<T, 2, 16, FORM, LAYER, POST, kSumPre, true><<<blocks, threads, 0, stream>>>(p);
+}
+template <typename T, Form FORM, bool LAYER, bool POST>
 void launch_form(const Join& p, hipStream_t stream) {
-  if (p.post_gain) (p.layer ? launch_all<T, C, FORM, true, true> : launch_all<T, C, FORM, false, true>)(p, stream);
-  else (p.layer ? launch_all<T, C, FORM, true, false> : launch_all<T, C, FORM, false, false>)(p, stream);
+  if (p.h <= 64 * 8) launch_all<T, 1, FORM, LAYER, POST>(p, stream);
+  else if (p.h <= 8 * 64 * 8 * 2) launch_all<T, 2, FORM, LAYER, POST>(p, stream);
+  else launch_wide<T, FORM, LAYER, POST>(p, stream);
+}
+template <typename T, Form FORM>
+void launch_form(const Join& p, hipStream_t stream) {
+  if (p.post_gain) (p.layer ? launch_form<T, FORM, true, true> : launch_form<T, FORM, false, true>)(p, stream);
+  else (p.layer ? launch_form<T, FORM, true, false> : launch_form<T, FORM, false, false>)(p, stream);
 }
 template <typename T>
 void launch_any(const Join& p, hipStream_t stream) {
-  const int blocks = blocks_of(p.rows, p.h);
-  if (p.h <= kMaxWaves * 64 * 8) {
-    norm_join_backward_kernel<T, 1, kAny, true, true, kSumPre | kSumPost | kSumGate, true><<<blocks, 64 * waves_of(p.h, 1), 0, stream>>>(p);
-    return;
-  }
-  const int threads = 64 * waves_of(p.h, 4);  // the sums first: dx may be dy, df dn
-  if (p.gate && !p.gate_per_value) norm_join_backward_kernel<T, 4, kAny, true, true, kSumGate, false><<<blocks, threads, 0, stream>>>(p);
-  if (p.post_gain) norm_join_backward_kernel<T, 4, kAny, true, true, kSumPost, false><<<blocks, threads, 0, stream>>>(p);
-  norm_join_backward_kernel<T, 4, kAny, true, true, kSumPre, true><<<blocks, threads, 0, stream>>>(p);
+  constexpr int ALL = kSumPre | kSumPost | kSumGate;
+  const int blocks = blocks_of(p.rows, p.h), threads = 64 * waves_of(p.h, 1);
+  if (p.h <= 8 * 64 * 8) norm_join_backward_kernel<T, 1, 8, kAny, true, true, ALL, true><<<blocks, threads, 0, stream>>>(p);
+  else if (p.h <= 16 * 64 * 8) norm_join_backward_kernel<T, 1, 16, kAny, true, true, ALL, true><<<blocks, threads, 0, stream>>>(p);
+  else launch_wide<T, kAny, true, true>(p, stream);
 }
 template <typename T>
 void launch_backward(const Join& p, hipStream_t stream) {
   const bool uses_f = p.post_gain || p.gate, pre = p.dn;
   const bool saved = (!pre || p.y_codes) && (!uses_f || p.f_codes), tensors = (!pre || p.y_in) && (!uses_f || p.f);
-  const int chunks = p.h <= 64 * 8 ? 1 : 2;
-  if (!p.vec || p.h > kMaxWaves * 64 * 8 * 2 || (!saved && !tensors)) return launch_any<T>(p, stream);
-  if (saved) (chunks == 1 ? launch_form<T, 1, kFromSaved> : launch_form<T, 2, kFromSaved>)(p, stream);
-  else (chunks == 1 ? launch_form<T, 1, kFromTensors> : launch_form<T, 2, kFromTensors>)(p, stream);
+  if (!p.vec || (!saved && !tensors)) return launch_any<T>(p, stream);
+  (saved ? launch_form<T, kFromSaved> : launch_form<T, kFromTensors>)(p, stream);
 }
 
 }  // namespace norm_join

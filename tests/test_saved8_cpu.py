@@ -1,12 +1,16 @@
 """8-bit checkpoints, host side: sizes, what the entry points refuse, the kernels' registers; the 64-bit reference against autograd."""
 import ctypes
+import json
 import math
+import os
+import re
 
 import pytest
 import torch
 
 import saved8_reference as ref
 from paper_2503_01328_amd import binding as po
+from paper_2503_01328_amd import build
 
 ROOM = 1 << 20
 AT = ctypes.addressof((ctypes.c_char * (ROOM + 4096)).from_buffer(bytearray(ROOM + 4096)))
@@ -197,3 +201,14 @@ def test_reference_slopes_are_autograds(silu, gated):
     torch.testing.assert_close(got["du"].v, u.grad)
     torch.testing.assert_close(got["out"].v, v.detach())
     torch.testing.assert_close(ref.activation_forward(u.detach(), silu, gated, torch.float32).v, v.detach())
+
+
+def test_kernels_keep_their_values_in_registers():
+    """But for norm backward kernels of rows that take sixteen waves, and of fp32 rows with every parameter, which do with some scratch."""
+    if not os.path.exists(build.RESOURCES):
+        pytest.skip("no resource report")
+    usage = json.load(open(build.RESOURCES))
+    names = [n for n in usage if any(k in n for k in ("saved8_kernel", "saved8_wide", "activation_", "norm_join", "weight_grad"))]
+    assert len(names) > 60
+    wide = re.compile(r"norm_join_backward_kernelI(DF16b|f)Li[12]ELi16E|norm_join_backward_kernelIfLi2ELi8E.*Li7E|norm_join_forward_kernelI(DF16b|f)Li4E")
+    assert not [n for n in names if usage[n]["ScratchSize"] > 0 and not wide.search(n)]
