@@ -431,7 +431,8 @@ int po_op_activation_backward(int32_t dtype, int32_t act, int32_t gated, const v
  *   n = N(y) * pre_gain + pre_shift (pre_gain and n NULL: no norm there)
  * N, a po_norm for both: (v - mean) / sqrt(var + eps) over a row, biased variance, or v / sqrt(mean(v^2) + eps), which has no shifts.  Gains and
  * shifts [h] of dtype, a shift may be NULL.  gate of dtype: [h] (gate_per_value 0) or [rows, h] (1).  saved_f, saved_y: NULL, or the checkpoints of f and
- * of y as it is stored.  y may be x, n may be f; what is written overlaps nothing else.  h 1 to 16384, 1 to 2^25 rows.
+ * of y as it is stored.  y may be x, n may be f; what is written overlaps nothing else.  h 1 to 16384, 1 to 2^25 rows, checkpoints of
+ * 2^31 values at most.
  * With post_gain and gate NULL and scales of 1 this is a layer's residual sum and LayerNorm. */
 typedef enum { PO_NORM_LAYER = 0, PO_NORM_RMS = 1 } po_norm;
 int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const void* f, const void* post_gain, const void* post_shift,
@@ -454,8 +455,8 @@ int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const 
 /* A weight's gradient from the checkpoint of its input: dw [k, n] fp32 (row stride ldc) = X^T dY (accumulate 0) or += (1), X [rows, k] as saved_x holds it,
  * dy [rows, n] of dtype (row stride ldy).  Exact products, fp32 sums, whatever dtype is, in an order that depends on the sizes alone.  dw overlaps neither
  * input.  workspace: po_op_weight_grad_saved8_workspace bytes (often 0: NULL will do), 16-byte aligned, contents unspecified before and
- * afterwards; one for more rows (of the same dtype, k and n) serves fewer.  1 to 2^25 rows, k and n 1 to 2^20 and 2^23 tiles of
- * 128 x 128 at most (beyond: PO_E_INVAL, and 0 bytes), ldy at most 2^22. */
+ * afterwards; one for more rows (of the same dtype, k and n) serves fewer.  1 to 2^25 rows, k and n 1 to 2^20, at most 2^21
+ * tiles of 128 x 128 and 2^31 values of X (beyond: PO_E_INVAL, and 0 bytes), ldy at most 2^22. */
 uint64_t po_op_weight_grad_saved8_workspace(int32_t dtype, int32_t rows, int32_t k, int32_t n);
 int po_op_weight_grad_saved8(int32_t dtype, const void* saved_x, const void* dy, int32_t ldy, float* dw, int32_t ldc, int32_t accumulate,
                              void* workspace, int32_t rows, int32_t k, int32_t n, void* stream);

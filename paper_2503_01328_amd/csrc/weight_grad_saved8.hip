@@ -1,7 +1,7 @@
 // A weight's gradient from the 8-bit checkpoint of its input:  dW [k, n] (+)= X^T dY,  X [rows, k] restored (saved8.h), dY [rows, n].
 //
 // A restored value is exact in bf16, so that the product belongs on the bf16 matrix cores whatever type dY has: in bf16 as it is, in
-// fp32 as the sum of three bf16 terms (8 + 8 + 8 significant bits, cut off rather than rounded, which makes the sum exact), three products of
+// fp32 as the sum of three bf16 terms (8 + 8 + 8 significant bits, cut off rather than rounded, which makes the sum exact down to 2^-126), three products of
 // exact operands with fp32 accumulators.  X never exists in 16 bits outside LDS.
 //
 // The contraction is over rows, the slow index of both operands: slices of 64 rows go through registers into LDS as [64][columns] bf16 (codes are
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256) void weight_grad_sum_kernel(WeightGrad p, int 
 }
 
 constexpr int kMaxRows = 1 << 25, kMaxWidth = 1 << 20, kMaxPitch = 1 << 22;  // a slice's offsets fit 31 bits
-constexpr int64_t kMaxTiles = 1 << 23;
+constexpr int64_t kMaxTiles = 1 << 21;
 
 struct Form {
   int tile, tiles_m, tiles_n, splits, split_rows;  // tile: 64, 128, or 256: the wide kernel
@@ -348,7 +348,7 @@ Form form_of(int dtype, int rows, int k, int n, bool wide) {
 }
 bool sizes_ok(int rows, int k, int n) {
   return rows >= 1 && rows <= kMaxRows && k >= 1 && k <= kMaxWidth && n >= 1 && n <= kMaxWidth &&
-         (int64_t)ceil_div(k, 128) * ceil_div(n, 128) <= kMaxTiles;
+         (int64_t)ceil_div(k, 128) * ceil_div(n, 128) <= kMaxTiles && saved8_codes(rows, k) / 8 <= kMaxSaved8Chunks;
 }
 
 template <typename T, int TILE, bool VEC>
@@ -387,9 +387,9 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
   const char* what = "weight_grad_saved8";
   const int size = dtype == kF32 ? 4 : 2;
   if (!sizes_ok(rows, k, n) || ldy < n || ldy > kMaxPitch || ldc < n || (accumulate != 0 && accumulate != 1)) {
-    set_error("%s: rows=%d k=%d n=%d ldy=%d ldc=%d accumulate=%d (1 to %d rows, k and n 1 to %d, at most %lld tiles of 128 x 128, ldy and "
+    set_error("%s: rows=%d k=%d n=%d ldy=%d ldc=%d accumulate=%d (1 to %d rows, k and n 1 to %d, rows x k at most %lld, at most %lld tiles of 128 x 128, ldy and "
               "ldc at least n, ldy at most %d, accumulate 0 or 1)", what, rows, k, n, ldy, ldc, accumulate, kMaxRows, kMaxWidth,
-              (long long)kMaxTiles, kMaxPitch);
+              (long long)kMaxSaved8Chunks * 8, (long long)kMaxTiles, kMaxPitch);
     return false;
   }
   const size_t needed = weight_grad_saved8_workspace(dtype, rows, k, n);

@@ -438,7 +438,9 @@ def _weight_grad(dtype, saved, dy, dw, accumulate, k, rows=None, n=None, workspa
 
 WEIGHTS = [(1, 1, 1), (1, 40, 24), (7, 33, 5), (63, 64, 64), (64, 64, 72), (65, 100, 130), (200, 128, 128), (129, 256, 1024), (1000, 96, 771), (257, 300, 264),
            (2000, 40, 56), (3000, 640, 256), (300, 2048, 2048), (130, 2056, 1544), (513, 1000, 4104),
-           (1, 2100, 3800), (64, 2048, 4096), (127, 2056, 3784), (129, 2100, 3801), (192, 2305, 3592), (700, 2100, 3800)]
+           (1, 2100, 3800), (64, 2048, 4096), (127, 2056, 3784), (129, 2100, 3801), (192, 2305, 3592), (700, 2100, 3800),
+           # many splits, few, results that are no whole vectors; large tiles aligned and not
+           (16384, 64, 64), (5000, 65, 77), (1500, 33, 35), (9000, 640, 256), (1733, 2048, 2048), (700, 2050, 2051), (4000, 1030, 1032)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -539,6 +541,57 @@ def test_weight_grad_special_values(gpu_device, dtype, rows, k, n, value):
         keep[7] = False  # the others of its block keep their own scale only where the value was not its largest
         keep[:32] = False
         assert torch.equal(got[keep], clean[keep])
+
+
+def test_weight_grad_offsets_past_32_bits(gpu_device):
+    """dy of 2^31 values and more; rows that hold something at both ends only."""
+    dev, rows, k, n = gpu_device, 70000, 40, 32768
+    x = torch.zeros(rows, k, dtype=torch.bfloat16, device=dev)
+    dy = torch.zeros(rows, n, dtype=torch.bfloat16, device=dev)
+    g = _gen(dev, 130)
+    some = torch.cat([torch.arange(3), torch.arange(rows - 5, rows)]).to(dev)
+    x[some] = torch.randint(-8, 9, (8, k), generator=g, device=dev).to(torch.bfloat16)
+    dy[some] = torch.randint(-100, 101, (8, n), generator=g, device=dev).to(torch.bfloat16)
+    dw = torch.empty(k, n, device=dev)
+    _weight_grad("bf16", _saved(x), dy, dw, 0, k)
+    assert torch.equal(dw.double(), x[some].double().T @ dy[some].double())
+
+
+def test_join_offsets_past_32_bits(gpu_device):
+    """Rows at the end of tensors of more than 2^31 values, forward and backward, against a call on those rows alone."""
+    dev, rows, h, last = gpu_device, 270000, 8192, 7
+    p = _params(dev, torch.bfloat16, h, rows, True, True, "columns")
+    x = torch.full((rows, h), 0.5, dtype=torch.bfloat16, device=dev)
+    f, y = torch.full_like(x, 0.25), torch.empty_like(x)
+    x[-last:], f[-last:] = _rand(dev, 131, last, h).to(x.dtype), _rand(dev, 132, last, h).to(x.dtype)
+    forward = lambda x, f, y, n: po.po_op_norm_join_forward(po.PO_BF16, po.PO_NORM_RMS, x, f, p["post_gain"], None, p["gate"], 0, p["skip"], p["branch"], p["pre_gain"],
+                                                           None, y, n, None, None, x.shape[0], h, p["eps"])
+    fx, ff = x[-last:].clone(), f[-last:].clone()
+    fy, fn = torch.empty_like(fx), torch.empty_like(fx)
+    forward(fx, ff, fy, fn)
+    forward(x, f, y, f)
+    assert torch.equal(y[-last:], fy) and torch.equal(f[-last:], fn)
+    assert torch.equal(y[0], y[rows // 2]) and torch.equal(f[0], f[rows - last - 1])
+
+    def backward(dy, dn, y, f):
+        sums = torch.zeros(3, h, device=dev)
+        ws = torch.empty(po.po_op_norm_join_backward_workspace(y.shape[0], h), dtype=torch.uint8, device=dev)
+        po.po_op_norm_join_backward(po.PO_BF16, po.PO_NORM_RMS, dy, dn, y, 0, f, 0, p["post_gain"], None, p["gate"], 0, p["skip"], p["branch"], p["pre_gain"], None,
+                                    dy, dn, sums[0], sums[1], None, sums[2], None, None, ws, y.shape[0], h, p["eps"])
+        return sums
+
+    dy, dn = torch.zeros_like(x), x  # (x is not needed again: the gradient of n, zero but at the end)
+    dn.zero_()
+    dy[-last:], dn[-last:] = _rand(dev, 133, last, h).to(x.dtype), _rand(dev, 134, last, h).to(x.dtype)
+    gy, gn = dy[-last:].clone(), dn[-last:].clone()
+    want = ref.join_backward(gy, gn, fy, ff, p | dict(pre_shift=None, post_shift=None), torch.bfloat16)
+    backward(gy, gn, fy, ff)
+    f[-last:] = ff
+    sums = backward(dy, dn, y, f)
+    assert torch.equal(dy[-last:], gy) and torch.equal(dn[-last:], gn)
+    assert not dy[:-last].any() and not dn[:-last].any()
+    for got, name in zip(sums, ("dgate", "dpost_gain", "dpre_gain")):  # the other rows add zeros
+        ref.check(got, want[name], name)
 
 
 # ---- together -----------------------------------------------------------------------------------------------------

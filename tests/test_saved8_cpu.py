@@ -106,12 +106,13 @@ def test_activation_backward_refuses(bad):
 JOIN = dict(dtype=po.PO_BF16, norm=0, x=at(0), f=at(1), post_gain=at(2), post_shift=at(3), gate=at(4), gate_per_value=0, skip=1.0, branch=1.0,
             pre_gain=at(5), pre_shift=at(6), y=at(7), n=at(8), saved_f=at(9), saved_y=at(10), rows=4, h=40, eps=1e-5)
 BAD_JOIN = [dict(dtype=5), dict(norm=2), dict(norm=-1), dict(norm=1), dict(rows=0), dict(rows=(1 << 25) + 1), dict(h=0), dict(h=16385), dict(skip=math.nan),
-            dict(branch=math.inf), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(gate_per_value=2), dict(post_gain=None), dict(pre_gain=None)]
+            dict(branch=math.inf), dict(rows=1 << 24, h=256), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(gate_per_value=2), dict(post_gain=None), dict(pre_gain=None)]
 
 
 @pytest.mark.parametrize("bad", BAD_JOIN + [dict(x=None), dict(f=None), dict(y=None), dict(n=None), dict(pre_gain=None, pre_shift=None), dict(x=at(0) + 1),
                                             dict(saved_f=at(9) + 8), dict(saved_y=at(9)), dict(y=at(1)), dict(n=at(0)), dict(n=at(7)), dict(y=at(0) + 2),
-                                            dict(saved_f=at(1)), dict(y=at(4) - 64), dict(n=at(5)), dict(gate=at(4), gate_per_value=1, y=at(4))], ids=str)
+                                            dict(saved_f=at(1)), dict(y=at(4) - 64), dict(n=at(5)), dict(gate=at(4), gate_per_value=1, y=at(4)), dict(y=at(0), gate=at(0)), dict(y=at(0), pre_gain=at(0)),
+                                            dict(n=at(1), post_shift=at(1)), dict(rows=1 << 25, h=9000, saved_f=None, saved_y=None)], ids=str)
 def test_join_forward_refuses(bad):
     _refused("dtype" if "dtype" in bad else "norm_join_forward", po.po_op_norm_join_forward, **{**JOIN, **bad})
 
@@ -126,7 +127,7 @@ BACK = dict(dtype=po.PO_BF16, norm=0, dy=at(0), dn=at(1), y=at(2), y_saved8=1, f
                                             dict(pre_shift=None), dict(post_shift=None), dict(workspace=None), dict(workspace=at(13) + 4),
                                             dict(dpre_gain=at(10) + 2), dict(y=at(2) + 8), dict(f=at(3) + 8), dict(dx=at(1)), dict(df=at(0)), dict(dx=at(2)),
                                             dict(df=at(3)), dict(dx=at(0) + 2), dict(n=at(1)), dict(n=at(5)), dict(dgate=at(8)), dict(dpre_gain=at(4)),
-                                            dict(workspace=at(6)), dict(dpre_shift=at(10) + 16), dict(y_saved8=0, dx=at(2)),
+                                            dict(workspace=at(6)), dict(dpre_shift=at(10) + 16), dict(y_saved8=0, dx=at(2)), dict(dx=at(0), gate=at(0)), dict(df=at(1), pre_gain=at(1)),
                                             dict(norm=1, post_shift=None, dpost_shift=None)], ids=str)
 def test_join_backward_refuses(bad):
     _refused("dtype" if "dtype" in bad else "norm_join_backward", po.po_op_norm_join_backward, **{**BACK, **bad})
@@ -136,7 +137,7 @@ WEIGHT = dict(dtype=po.PO_BF16, saved_x=at(0), dy=at(2), ldy=24, dw=at(4), ldc=2
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=9), dict(rows=0), dict(rows=(1 << 25) + 1), dict(k=0), dict(k=(1 << 20) + 1), dict(n=0), dict(n=25), dict(ldy=23), dict(ldy=(1 << 22) + 1),
-                                 dict(ldc=23), dict(k=1 << 20, n=1 << 20, ldy=1 << 20, ldc=1 << 20), dict(accumulate=2), dict(saved_x=None), dict(dy=None),
+                                 dict(ldc=23), dict(k=1 << 20, n=1 << 20, ldy=1 << 20, ldc=1 << 20), dict(k=1 << 18, n=1 << 18, ldy=1 << 18, ldc=1 << 18), dict(rows=1 << 20, k=2080), dict(accumulate=2), dict(saved_x=None), dict(dy=None),
                                  dict(dw=None), dict(saved_x=at(0) + 8), dict(dy=at(2) + 1), dict(dw=at(4) + 2), dict(dw=at(0)), dict(dw=at(2) + 32),
                                  dict(rows=20000, workspace=None), dict(rows=2000, workspace=at(6) + 8), dict(rows=600, workspace=at(4))], ids=str)
 def test_weight_grad_refuses(bad):
