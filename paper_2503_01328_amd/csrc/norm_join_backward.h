@@ -3,7 +3,8 @@
 // A block takes rows one after another.  Each tensor's registers are loaded with the next row's values, packed as they lie in memory, as soon as
 // this row's have been used, so that a row's loads are under way while the row before is computed; parameters stay in registers.
 // Loads and stores go through buffers that end with the row: columns behind it, tensors that are not there and rows behind the last read
-// as zeros without a branch (branches around loads made the compiler wait for each at once: 4096 rows of 4096, LayerNorm, 50 us).
+// as zeros without a branch: branches around loads made the compiler wait for each at once (16384 rows of 5120, both norms and a gate: 435 us, without 228).
+// What bounds it: memory, 5.4 TB/s in that case with the blocks that the chip holds at once (212 us).
 #pragma once
 
 #include "norm_join.h"

@@ -5,7 +5,11 @@
 // exact operands with fp32 accumulators.  X never exists in 16 bits outside LDS.
 //
 // The contraction is over rows, the slow index of both operands: slices of 64 rows go through registers into LDS as [64][columns] bf16 (codes are
-// scaled on the way, sixteen columns of a row have one scale), and the fragments come out of it by transposing reads.
+// scaled on the way: a row's neighbouring columns have one scale), and the fragments come out of it by transposing reads.
+//
+// Large bf16 results: gemm_wide_tile.h's pipeline, bound by the matrix cores (4096 rows, 4096 x 16384: 457 us, 1.20 PFLOP/s; a plain product of 8192^3
+// 1.34).  Others: tiles of 128 and 64, bound by LDS, which a slice of 128 x 128 keeps busy for half of its 0.77 us (1733 rows, 2048 x 2048: 30 us; fp32 59), small
+// ones by the chain of slices (16384 rows, 640 x 256: 18 us and 4 for the sum of the splits).
 #include <algorithm>
 
 #include "gemm_tile.h"
@@ -98,7 +102,8 @@ __device__ __forceinline__ int eight_at(int row, int eight) {  // byte of eight 
   return row * (2 * TILE) + (((eight >> 1) ^ (row & MASK)) << 5) + ((eight & 1) << 4);
 }
 
-// TILE x TILE results a block, WAVES waves, two of them down.  AHEAD slices are on their way into registers while one is computed: a slice is
+// TILE x TILE results a block, WAVES waves in two rows (128: eight of 64 x 32, two to a SIMD; 1733 rows, 2048 x 2048, with four of 64 x 64 35 us, so 32).
+// AHEAD slices are on their way into registers while one is computed: a slice is
 // 512 cycles of MFMAs (TILE 128), memory a thousand and more away.
 template <typename T, int TILE, bool VEC, int AHEAD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void weight_grad_saved8_kernel(WeightGrad p) {
