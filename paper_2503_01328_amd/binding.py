@@ -122,8 +122,8 @@ EXPORTS = {
     "po_op_pack": (C.c_int, [C.POINTER(C.c_void_p), C.POINTER(C.c_uint64), C.c_int32, C.c_void_p, C.c_void_p]),
     "po_op_unpack": (C.c_int, [C.POINTER(C.c_void_p), C.POINTER(C.c_uint64), C.c_int32, C.c_void_p, C.c_void_p]),
     "po_op_saved8_bytes": (C.c_uint64, [C.c_int32, C.c_int32]),
-    "po_op_save8": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_void_p)] + [C.POINTER(C.c_int32)] * 3 + [C.POINTER(C.c_void_p), C.c_void_p]),
-    "po_op_restore8": (C.c_int, [C.c_int32, C.c_int32, C.POINTER(C.c_void_p)] + [C.POINTER(C.c_int32)] * 3 + [C.POINTER(C.c_void_p), C.c_void_p]),
+    "po_op_save8": (C.c_int, [C.c_int32, C.c_int32] + [C.c_void_p] * 6),
+    "po_op_restore8": (C.c_int, [C.c_int32, C.c_int32] + [C.c_void_p] * 6),
     "po_op_activation_forward": (C.c_int, [C.c_int32] * 3 + [C.c_void_p] * 3 + [C.c_int32, C.c_int32, C.c_void_p]),
     "po_op_activation_backward": (C.c_int, [C.c_int32] * 3 + [C.c_void_p, C.c_int32] + [C.c_void_p] * 3 + [C.c_int32, C.c_int32, C.c_void_p]),
     "po_op_norm_join_forward": (C.c_int, [C.c_int32] * 2 + [C.c_void_p] * 5 + [C.c_int32, C.c_float, C.c_float] + [C.c_void_p] * 6 +
@@ -424,40 +424,50 @@ def po_op_saved8_bytes(rows, cols) -> int:
     return lib.po_op_saved8_bytes(rows, cols)
 
 
-# Array types by length: making one anew takes longer than filling it.
-_I32 = [C.c_int32 * n for n in range(9)]
-_VOIDP = [C.c_void_p * n for n in range(9)]
+# Array types by number of tensors (making one anew takes longer than filling it): rows, cols and row strides of them, pointers of them and their
+# checkpoints, in one array each.
+_SIZES = [C.c_int32 * (3 * n) for n in range(9)]
+_POINTERS = [C.c_void_p * (2 * n) for n in range(9)]
 
 
 def _matrices(tensors, saved):
-    """(n, pointers, rows, cols, row strides, checkpoints) of 2-d tensors with neighbouring columns, or of tuples of the first four, as C arrays."""
+    """2-d tensors with neighbouring columns, or tuples (pointer, rows, cols, row stride), and their checkpoints: (n, sizes, pointers), C arrays."""
     n = len(tensors)
     if len(saved) != n:
         raise ValueError("a checkpoint for every tensor is needed")
-    given = []
+    at, rows, cols, strides = [], [], [], []
     for t in tensors:
-        if type(t) is not tuple:
-            rows, cols = t.shape
+        if type(t) is tuple:
+            p, r, c, ld = t
+        else:
+            r, c = t.shape
             ld, inner = t.stride()
-            if inner != 1 and cols > 1:
+            if inner != 1 and c > 1:
                 raise ValueError("the columns of a row have to be neighbours")
-            t = (t.data_ptr(), rows, cols, ld if rows > 1 else cols)
-        given.append(t)
-    ints, pointers = (_I32[n], _VOIDP[n]) if n <= 8 else (C.c_int32 * n, C.c_void_p * n)
-    x, rows, cols, ld = zip(*given) if given else ((),) * 4
-    return n, pointers(*x), ints(*rows), ints(*cols), ints(*ld), pointers(*[_ptr(s) for s in saved])
+            if r <= 1:
+                ld = c
+            p = t.data_ptr()
+        at.append(p)
+        rows.append(r)
+        cols.append(c)
+        strides.append(ld)
+    at += [s if s is None or type(s) is int else s.data_ptr() for s in saved]
+    sizes, pointers = (_SIZES[n], _POINTERS[n]) if n <= 8 else (C.c_int32 * (3 * n), C.c_void_p * (2 * n))
+    return n, sizes(*rows, *cols, *strides), pointers(*at)
 
 
 def po_op_save8(dtype, tensors, saved, stream=None):
     """tensors: list of 2-d tensors (rows may have a stride) or (pointer, rows, cols, row stride); saved: their checkpoints' buffers."""
-    n, x, rows, cols, ld, to = _matrices(tensors, saved)
-    _check(lib.po_op_save8(dtype, n, x, rows, cols, ld, to, _stream(stream)))
+    n, sizes, pointers = _matrices(tensors, saved)
+    s, p = C.addressof(sizes), C.addressof(pointers)
+    _check(lib.po_op_save8(dtype, n, p, s, s + 4 * n, s + 8 * n, p + 8 * n, _stream(stream)))
 
 
 def po_op_restore8(dtype, saved, tensors, stream=None):
     """saved, tensors: as for po_op_save8."""
-    n, x, rows, cols, ld, at = _matrices(tensors, saved)
-    _check(lib.po_op_restore8(dtype, n, at, rows, cols, ld, x, _stream(stream)))
+    n, sizes, pointers = _matrices(tensors, saved)
+    s, p = C.addressof(sizes), C.addressof(pointers)
+    _check(lib.po_op_restore8(dtype, n, p + 8 * n, s, s + 4 * n, s + 8 * n, p, _stream(stream)))
 
 
 def po_op_activation_forward(dtype, act, gated, u, out, saved_u, rows, f, stream=None):

@@ -352,6 +352,32 @@ def test_join_without_what_may_be_left_out(gpu_device, dtype, rms):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,h", [(40, 264), (700, 2048), (9, 8200), (33, 517)])
+def test_join_from_checkpoints_and_from_what_they_hold(gpu_device, dtype, rows, h):
+    """y and f from checkpoints, from tensors of the same values, one of each."""
+    dev, (code, tdt) = gpu_device, DT[dtype]
+    p = _params(dev, tdt, h, rows, False, True, "columns")
+    dy, dn = _rand(dev, 56, rows, h, dtype=tdt), _rand(dev, 57, rows, h, dtype=tdt)
+    saved = [_saved(_rand(dev, 58 + k, rows, h, dtype=tdt)) for k in range(2)]
+    held = [torch.empty(rows, h, dtype=tdt, device=dev) for _ in range(2)]
+    po.po_op_restore8(code, saved, held)
+    want = ref.join_backward(dy, dn, *held, p, tdt)
+    results = []
+    for ys in (0, 1):
+        for fs in (0, 1):
+            dx, df = torch.empty_like(dy), torch.empty_like(dy)
+            sums = torch.zeros(5, h, device=dev)
+            ws = torch.empty(po.po_op_norm_join_backward_workspace(rows, h), dtype=torch.uint8, device=dev)
+            po.po_op_norm_join_backward(code, _norm_kind(p), dy, dn, (held, saved)[ys][0], ys, (held, saved)[fs][1], fs, p["post_gain"], p["post_shift"], p["gate"], 0,
+                                        p["skip"], p["branch"], p["pre_gain"], p["pre_shift"], dx, df, sums[4], sums[0], sums[1], sums[2], sums[3], None, ws, rows, h,
+                                        p["eps"])
+            results.append((dx, df, sums))
+            for k, t in dict(dx=dx, df=df, dpost_gain=sums[0], dpost_shift=sums[1], dpre_gain=sums[2], dpre_shift=sums[3], dgate=sums[4]).items():
+                ref.check(t, want[k], f"{k}, y saved {ys}, f saved {fs}")
+    assert all(torch.equal(a, b) for a, b in zip(results[0], results[3]))  # the same arithmetic on the same numbers
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_join_in_place(gpu_device, dtype):
     dev, (code, tdt), rows, h = gpu_device, DT[dtype], 33, 264
     p = _params(dev, tdt, h, rows, False, True, "columns")
