@@ -319,7 +319,7 @@ __device__ __forceinline__ void gemm_tile(int M, int N, int K, OperandA A, int l
   int m0 = tile_m * BM, n0 = tile_n * BN;
 
   constexpr bool SAVED = std::is_same<OperandA, Saved8Operand>::value;
-  static_assert(!SAVED || (TA && EDGE && stages_of(WTM, WTN) == 2), "the form that a checkpoint's slices are woven into");
+  static_assert(!SAVED || (TA && EDGE), "the form that a checkpoint's slices are woven into");
   const bf16* a_base = nullptr;
   if constexpr (!SAVED) a_base = TA ? A + m0 : A + (size_t)m0 * lda;
   const bf16* b_base = TB ? B + n0 : B + (size_t)n0 * ldb;
@@ -340,7 +340,7 @@ __device__ __forceinline__ void gemm_tile(int M, int N, int K, OperandA A, int l
   //   barrier      one per slice, before k-step 1: it publishes slice kt + 1 (whose first fragments are read
   //                from k-step 1 on) and releases stage kt % NSTAGE (whose last fragments were read in k-step 0).
   // The big tiles have room for two stages, the small tile (a slice is four times shorter) gets four.
-  constexpr int NSTAGE = stages_of(WTM, WTN);
+  constexpr int NSTAGE = SAVED ? 2 : stages_of(WTM, WTN);
   using LoaderA = typename std::conditional<SAVED, Saved8SliceLoader<SAVED ? BM : 128>, SliceLoader<BM, TA, EDGE>>::type;
   using LoaderB = SliceLoader<BN, TB, EDGE>;
   constexpr int PER_SLICE = LoaderA::PER_WAVE + LoaderB::PER_WAVE;  // load instructions of one wave per slice

@@ -7,8 +7,8 @@
 // The contraction is over rows, the slow index of both operands: slices of 64 rows go through registers into LDS as [64][columns] bf16 (codes are
 // scaled on the way: a row's neighbouring columns have one scale), and the fragments come out of it by transposing reads.
 //
-// Large bf16 results: gemm_wide_tile.h's pipeline, bound by the matrix cores (4096 rows, 4096 x 16384: 457 us, 1.20 PFLOP/s; a plain product of 8192^3
-// 1.34).  Others: tiles of 128 and 64, bound by LDS, which a slice of 128 x 128 keeps busy for half of its 0.77 us (1733 rows, 2048 x 2048: 30 us; fp32 59), small
+// Large and long bf16 results: gemm_wide_tile.h's pipeline in tiles of 256 x 256 and 128 x 256, bound by the matrix cores (4096 rows, 4096 x 16384: 457 us, 1.20
+// PFLOP/s, a plain product of 8192^3 1.34; 4096 x 2048: 71 us, 0.97).  Others: tiles of 128 and 64, bound by LDS, which a slice of 128 x 128 keeps busy for half of its 0.77 us (1733 rows, 2048 x 2048: 30 us; fp32 59), small
 // ones by the chain of slices (16384 rows, 640 x 256: 18 us and 4 for the sum of the splits).
 #include <algorithm>
 
@@ -322,29 +322,39 @@ __global__ __launch_bounds__(256) void weight_grad_sum_kernel(WeightGrad p, int 
 constexpr int kMaxRows = 1 << 25, kMaxWidth = 1 << 20, kMaxPitch = 1 << 22;  // a slice's offsets fit 31 bits
 constexpr int64_t kMaxTiles = 1 << 21;
 
-struct Form {
-  int tile, tiles_m, tiles_n, splits, split_rows;  // tile: 64, 128, or 256: the wide kernel
+// The tiles there are: rows of dW (k), columns, whether of the wide kernel, blocks of a round, us a slice of a full round in bf16 and fp32 (measured).
+// 4096 rows, 4096 x 2048: 128 x 256 73 us, 128 x 128 94 (256 x 128, which the checkpoint's conversions slow down, 80).
+struct Tile {
+  int m, n;
+  bool wide;
+  int round;
+  double slice_bf16, slice_f32;
 };
-// At most so many splits: a round of blocks (two of the small ones to a CU), four slices each at least.
-int most_splits(int rows, int64_t tiles, int tile) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * kSlice), (tile == 128 ? 256 : 512) / tiles));
+constexpr Tile kTiles[] = {{64, 64, false, 512, 0.55, 1.5}, {128, 128, false, 256, 0.77, 1.9}, {128, 256, true, 256, 1.05, 0}, {256, 256, true, 256, 1.7, 0}};
+struct Form {
+  int tile, tiles_m, tiles_n, splits, split_rows;  // tile: of kTiles
+};
+int64_t tiles_of(const Tile& t, int k, int n) { return (int64_t)ceil_div(k, t.m) * ceil_div(n, t.n); }
+// At most so many splits: a round of blocks, four slices each at least.
+int most_splits(const Tile& t, int rows, int k, int n) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * kSlice), t.round / tiles_of(t, k, n)));
 }
 // The tile and the splits that should take least: rounds of blocks, each its slices one after another, a split's partial results written and
-// read again.  Measured, us a slice of a full round: bf16 0.77 (128 x 128, 256 blocks), 0.55 (64 x 64, 512 blocks), fp32 1.9 and 1.5; the sum 3 and 8
-// bytes a partial result at 5 TB/s.  The wide kernel from 128 of its tiles on: a round of 256 takes 1.7 a slice, for four times the work.
+// read again (the sum 3 us and 8 bytes a partial result at 5 TB/s).
 Form form_of(int dtype, int rows, int k, int n, bool wide) {
-  if (wide && (int64_t)ceil_div(k, 256) * ceil_div(n, 256) >= 128) return Form{256, ceil_div(k, 256), ceil_div(n, 256), 1, rows};
   Form best = {};
   double least = 0;
-  for (int tile = 64; tile <= 128; tile *= 2) {
-    const int64_t tiles = (int64_t)ceil_div(k, tile) * ceil_div(n, tile), round = tile == 128 ? 256 : 512;
-    const double slice = tile == 128 ? (dtype == kF32 ? 1.9 : 0.77) : (dtype == kF32 ? 1.5 : 0.55);
-    for (int splits = most_splits(rows, tiles, tile);; splits /= 2) {
+  for (int tile = 0; tile < 4; ++tile) {
+    const Tile& t = kTiles[tile];
+    if (t.wide && !wide) continue;
+    const int64_t tiles = tiles_of(t, k, n);
+    for (int splits = most_splits(t, rows, k, n);; splits /= 2) {
       const int each = ceil_div(ceil_div(rows, splits), kSlice);  // slices
-      const double time = (double)ceil_div64(tiles * splits, round) * (each + 4) * slice + (splits > 1 ? 3 + splits * (double)k * n * 8 / 5e6 : 0);
-      if (best.tile == 0 || time < least) {
+      const double time = (double)ceil_div64(tiles * splits, t.round) * (each + 4) * (dtype == kF32 ? t.slice_f32 : t.slice_bf16) +
+                          (splits > 1 ? 3 + splits * (double)k * n * 8 / 5e6 : 0);
+      if (least == 0 || time < least) {
         least = time;
-        best = Form{tile, ceil_div(k, tile), ceil_div(n, tile), ceil_div(rows, each * kSlice), each * kSlice};
+        best = Form{tile, ceil_div(k, t.m), ceil_div(n, t.n), ceil_div(rows, each * kSlice), each * kSlice};
       }
       if (splits <= 1) break;
     }
@@ -366,24 +376,29 @@ bool launch(const WeightGrad& p, const Form& f, hipStream_t stream) {
 }
 template <typename T>
 bool launch(const WeightGrad& p, const Form& f, bool vec, hipStream_t stream) {
-  return (f.tile == 128 ? (vec ? launch<T, 128, true> : launch<T, 128, false>) : (vec ? launch<T, 64, true> : launch<T, 64, false>))(p, f, stream);
+  return (f.tile == 1 ? (vec ? launch<T, 128, true> : launch<T, 128, false>) : (vec ? launch<T, 64, true> : launch<T, 64, false>))(p, f, stream);
+}
+template <int WTM, int WTN, int EPI>
+bool launch_wide(const WeightGrad& p, const Form& f, hipStream_t stream) {
+  constexpr int BYTES = 2 * 64 * (WTM + WTN) * 128;
+  static LdsLimit limit;
+  if (!limit.allow(weight_grad_saved8_wide_kernel<WTM, WTN, EPI>, BYTES)) return false;
+  weight_grad_saved8_wide_kernel<WTM, WTN, EPI><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 256, BYTES, stream>>>(p);
+  return launch_ok("weight_grad_saved8_wide_kernel");
 }
 template <int EPI>
 bool launch_wide(const WeightGrad& p, const Form& f, hipStream_t stream) {
-  constexpr int BYTES = stages_of(4, 4) * (256 + 256) * 128;
-  static LdsLimit limit;
-  if (!limit.allow(weight_grad_saved8_wide_kernel<4, 4, EPI>, BYTES)) return false;
-  weight_grad_saved8_wide_kernel<4, 4, EPI><<<dim3((unsigned)(f.tiles_m * f.tiles_n), (unsigned)f.splits), 256, BYTES, stream>>>(p);
-  return launch_ok("weight_grad_saved8_wide_kernel");
+  return (f.tile == 2 ? launch_wide<2, 4, EPI> : launch_wide<4, 4, EPI>)(p, f, stream);
 }
 
 }  // namespace
 
 size_t weight_grad_saved8_workspace(int dtype, int rows, int k, int n) {
   if (!sizes_ok(rows, k, n)) return 0;
-  // for the most splits that either tile may take, so that a workspace for more rows serves fewer
+  // for the most splits that any tile may take, so that a workspace for more rows serves fewer
   int most = 1;
-  for (int tile = 64; tile <= 128; tile *= 2) most = std::max(most, most_splits(rows, (int64_t)ceil_div(k, tile) * ceil_div(n, tile), tile));
+  for (const Tile& t : kTiles)
+    if (!t.wide || dtype == kBF16) most = std::max(most, most_splits(t, rows, k, n));
   return most > 1 ? (size_t)most * k * n * sizeof(float) : 0;
 }
 
@@ -432,8 +447,10 @@ bool weight_grad_saved8(int dtype, const void* saved_x, const void* dy, int ldy,
   p.tiles_n = f.tiles_n;
   p.split_rows = f.split_rows;
   p.vec_w = vec_w;
-  if (f.tile == 256) return accumulate ? launch_wide<kEpiAccumulate>(p, f, stream) : launch_wide<kEpiStoreF32>(p, f, stream);
-  if (!(dtype == kF32 ? launch<float> : launch<bf16>)(p, f, vec_y && n % (16 / size) == 0, stream)) return false;
+  const bool done = kTiles[f.tile].wide ? (accumulate && f.splits == 1 ? launch_wide<kEpiAccumulate>(p, f, stream) : launch_wide<kEpiStoreF32>(p, f, stream))
+                    : dtype == kF32     ? launch<float>(p, f, vec_y && n % 4 == 0, stream)
+                                        : launch<bf16>(p, f, vec_y && n % 8 == 0, stream);
+  if (!done) return false;
   if (f.splits == 1) return true;
   const bool many = f.splits > 8, whole = (int64_t)k * n % 4 == 0;
   const unsigned blocks = (unsigned)ceil_div64((int64_t)k * n, many ? 128 : 1024);

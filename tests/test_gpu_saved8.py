@@ -466,7 +466,9 @@ WEIGHTS = [(1, 1, 1), (1, 40, 24), (7, 33, 5), (63, 64, 64), (64, 64, 72), (65, 
            (2000, 40, 56), (3000, 640, 256), (300, 2048, 2048), (130, 2056, 1544), (513, 1000, 4104),
            (1, 2100, 3800), (64, 2048, 4096), (127, 2056, 3784), (129, 2100, 3801), (192, 2305, 3592), (700, 2100, 3800),
            # many splits, few, results that are no whole vectors; large tiles aligned and not
-           (16384, 64, 64), (5000, 65, 77), (1500, 33, 35), (9000, 640, 256), (1733, 2048, 2048), (700, 2050, 2051), (4000, 1030, 1032)]
+           (16384, 64, 64), (5000, 65, 77), (1500, 33, 35), (9000, 640, 256), (1733, 2048, 2048), (700, 2050, 2051), (4000, 1030, 1032),
+           # wide tiles with splits
+           (2391, 136, 6368), (3414, 7120, 528), (12171, 496, 2320)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
