@@ -54,29 +54,35 @@ struct Planes<float> {
   static constexpr int N = 3;
 };
 
-// Eight columns of a row of dY in registers, and from there into their planes.  Loads go through a buffer that ends with the slice's rows; a column
-// that is not there is asked for past its end.  VEC: 16-byte pieces that are all there or not at all.
+// Eight columns of a row of dY in registers, and from there into their planes.  VEC: 16-byte pieces that are all there or not at all; loads go through
+// a buffer that ends with the slice's rows, and a piece that is not there is asked for past its end.
 template <typename T, bool VEC>
 struct Eight {
   static constexpr int V = 8 * sizeof(T) / 16;  // 16-byte pieces
   u32x4 v[V];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t slice, int at, int held) {  // at: bytes; held: columns that there are
-    if constexpr (VEC) {
-      constexpr int E = 16 / sizeof(T);
+  // at: bytes from the slice's first; held: columns that there are
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t slice, int at, int held) {
+    constexpr int E = 16 / sizeof(T);
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(slice, i * E < held ? at + 16 * i : (int)kOutOfBuffer, 0, 0));
+    for (int i = 0; i < V; ++i)
+      v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(slice, i * E < held ? at + 16 * i : (int)kOutOfBuffer, 0, 0));
+  }
+  // From rows on no 16-byte boundaries: whole vectors from wherever they start, past the end of a row too (what is there meets only results that are not
+  // written), and single values at the end of the last row (1512 rows, 7824 x 285: 33 us, with single values everywhere 69).
+  // there: whether dY has the row and the first column; left: bytes from the slice's first to dY's last.
+  __device__ __forceinline__ void load(const uint8_t* slice, int at, int held, bool there, int64_t left) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (!there) return;
+    if (at + (int64_t)(8 * sizeof(T)) <= left) {
+      __builtin_memcpy(v, slice + at, 8 * sizeof(T));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int from = i < held ? at + i * (int)sizeof(T) : (int)kOutOfBuffer;
-        if constexpr (sizeof(T) == 4) {
-          v[i / 4][i % 4] = __builtin_amdgcn_raw_buffer_load_b32(slice, from, 0, 0);
-        } else {
-          const unsigned e = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(slice, from, 0, 0);
-          v[0][i / 2] = i % 2 ? v[0][i / 2] | e << 16 : e;
+      for (int i = 0; i < 8; ++i)
+        if (i < held) {
+          if constexpr (sizeof(T) == 4) v[i / 4][i % 4] = reinterpret_cast<const unsigned*>(slice + at)[i];
+          else v[0][i / 2] |= (unsigned)reinterpret_cast<const uint16_t*>(slice + at)[i] << (16 * (i % 2));
         }
-      }
     }
   }
   // plane pl's 16 bytes
@@ -136,14 +142,18 @@ __global__ __launch_bounds__(64 * WAVES) void weight_grad_saved8_kernel(WeightGr
     const int64_t at = (int64_t)r0 * p.padded;
     const __amdgpu_buffer_rsrc_t x = buffer_resource(p.codes + at, rows * p.padded);
     const __amdgpu_buffer_rsrc_t scale = buffer_resource(p.scales + (at >> 5), rows * p.padded >> 5);
-    const __amdgpu_buffer_rsrc_t slice =
-        buffer_resource((const uint8_t*)p.dy + (int64_t)r0 * p.ldy * (int)sizeof(T), rows * p.ldy * (int)sizeof(T));
+    const uint8_t* dy = (const uint8_t*)p.dy + (int64_t)r0 * p.ldy * (int)sizeof(T);
+    const __amdgpu_buffer_rsrc_t slice = buffer_resource(dy, rows * p.ldy * (int)sizeof(T));
+    const int64_t left = ((int64_t)(p.rows - 1 - r0) * p.ldy + p.n) * (int)sizeof(T);
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const auto q = __builtin_amdgcn_raw_buffer_load_b64(x, x_at[u] >= 0 ? x_at[u] : (int)kOutOfBuffer, 0, 0);
       codes[slot][u] = make_uint2(q[0], q[1]);
       byte[slot][u] = __builtin_amdgcn_raw_buffer_load_b8(scale, x_at[u] >= 0 ? x_at[u] >> 5 : (int)kOutOfBuffer, 0, 0);
-      y[slot][u].load(slice, y_at[u], y_held[u]);
+      if constexpr (VEC)
+        y[slot][u].load(slice, y_at[u], y_held[u]);
+      else
+        y[slot][u].load(dy, y_at[u], y_held[u], (u * (64 * WAVES) + tid) / EIGHTS < rows && y_held[u] > 0, left);
     }
   };
   auto stage = [&](int slot, int u, char* lds) {

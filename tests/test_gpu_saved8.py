@@ -538,7 +538,7 @@ def test_weight_grad_workspace_kept_from_more_rows(gpu_device, dtype):
 
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, 3.3e38])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,k,n", [(100, 48, 64), (300, 2048, 1152), (90, 2100, 3800)])
+@pytest.mark.parametrize("rows,k,n", [(100, 48, 64), (300, 2048, 1152), (90, 2100, 3800), (1500, 33, 133), (700, 2050, 2051)])
 def test_weight_grad_special_values(gpu_device, dtype, rows, k, n, value):
     """One value that is not finite, or near the largest, in dy: its column alone, with the infinity that the formula has; in X: its row alone."""
     dev, tdt = gpu_device, DT[dtype][1]
