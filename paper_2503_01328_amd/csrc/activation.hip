@@ -27,7 +27,6 @@ struct Act {
   uint32_t chunks, row_chunks;  // eights of columns of out, padded to blocks, altogether and in a row
   int rows, f, cols;            // columns of out, of u
   int padded;                   // codes in a row
-  int vec;
 };
 
 // The activation and its slope in terms of the gate keep = e r, r = 1 / (1 + e): e = exp(2 z) for GeLU, exp(a) for SiLU, r = 1 - keep.  As e r
@@ -64,8 +63,8 @@ __global__ __launch_bounds__(256) void activation_forward_kernel(Act p) {
     col[k] = (i - row[k] * p.row_chunks) * 8;
     const int held = i < p.chunks ? p.f - (int)col[k] : 0;
     const T* u = (const T*)p.u + (size_t)row[k] * p.cols + col[k];
-    load_eight(a[k], u, held, p.vec && held >= 8);
-    if (GATED) load_eight(b[k], u + b_at, held, p.vec && held >= 8);
+    load_eight(a[k], u, held);
+    if (GATED) load_eight(b[k], u + b_at, held);
   }
 #pragma unroll
   for (int k = 0; k < UNROLL; ++k) {
@@ -93,7 +92,7 @@ __global__ __launch_bounds__(256) void activation_forward_kernel(Act p) {
       a[k][e] = act_of<SILU>(a[k][e]);
       if (GATED) a[k][e] *= b[k][e];
     }
-    if (there) store_eight((T*)p.out + (size_t)row[k] * p.f + col[k], a[k], held, p.vec && held >= 8);
+    if (there) store_eight((T*)p.out + (size_t)row[k] * p.f + col[k], a[k], held);
   }
 }
 
@@ -106,7 +105,6 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(Act p) {
   for (int k = 0; k < UNROLL; ++k) {
     const uint32_t i = base + 256u * k, row = i / p.row_chunks, col = (i - row * p.row_chunks) * 8;
     const int held = i < p.chunks ? p.f - (int)col : 0;
-    const bool whole = p.vec && held >= 8;
     if (SAVED) {
       const size_t at = (size_t)row * p.padded + col;
       uint2 ca = make_uint2(0, 0), cb = ca;
@@ -123,17 +121,16 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(Act p) {
       if (GATED) saved8_decode(cb, bb, b[k]);
     } else {
       const T* u = (const T*)p.u + (size_t)row * p.cols + col;
-      load_eight(a[k], u, held, whole);
-      if (GATED) load_eight(b[k], u + b_at, held, whole);
+      load_eight(a[k], u, held);
+      if (GATED) load_eight(b[k], u + b_at, held);
     }
-    load_eight(d[k], (const T*)p.d_out + (size_t)row * p.f + col, held, whole);
+    load_eight(d[k], (const T*)p.d_out + (size_t)row * p.f + col, held);
   }
 #pragma unroll
   for (int k = 0; k < UNROLL; ++k) {
     const uint32_t i = base + 256u * k, row = i / p.row_chunks, col = (i - row * p.row_chunks) * 8;
     if (i >= p.chunks) continue;
     const int held = p.f - (int)col;
-    const bool whole = p.vec && held >= 8;
     T* du = (T*)p.du + (size_t)row * p.cols + col;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -148,12 +145,12 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(Act p) {
         d[k][e] *= slope;
       }
     }
-    if (p.out) store_eight((T*)p.out + (size_t)row * p.f + col, a[k], held, whole);
+    if (p.out) store_eight((T*)p.out + (size_t)row * p.f + col, a[k], held);
     if (GATED) {
-      store_eight(du, b[k], held, whole);
-      store_eight(du + b_at, d[k], held, whole);
+      store_eight(du, b[k], held);
+      store_eight(du + b_at, d[k], held);
     } else {
-      store_eight(du, d[k], held, whole);
+      store_eight(du, d[k], held);
     }
   }
 }
@@ -232,10 +229,6 @@ Act shape_of(int dtype, int gated, int rows, int f) {
   p.chunks = p.row_chunks * (uint32_t)rows;
   return p;
 }
-bool aligned(uint64_t pointers, int dtype, const Act& p) {
-  const int size = dtype == kF32 ? 4 : 2;
-  return pointers % 16 == 0 && (p.rows == 1 ? p.cols == p.f || (int64_t)p.f * size % 16 == 0 : (int64_t)p.f * size % 16 == 0);
-}
 
 }  // namespace
 
@@ -265,7 +258,6 @@ bool activation_forward(int dtype, int act, int gated, const void* u, void* out,
     p.codes_out = (uint8_t*)saved_u;
     p.scales_out = p.codes_out + saved8_codes(rows, p.cols);
   }
-  p.vec = aligned((uintptr_t)u | (uintptr_t)out, dtype, p);
   auto k = dtype == kF32 ? (silu ? (gated ? launch_forward<float, true, true> : launch_forward<float, true, false>)
                                  : (gated ? launch_forward<float, false, true> : launch_forward<float, false, false>))
                          : (silu ? (gated ? launch_forward<bf16, true, true> : launch_forward<bf16, true, false>)
@@ -307,7 +299,6 @@ bool activation_backward(int dtype, int act, int gated, const void* u, int u_sav
     (dtype == kF32 ? launch_ragged<float, true> : launch_ragged<bf16, true>)(p, silu, stream);
     return launch_ok("activation_ragged_kernel");
   }
-  p.vec = aligned((uintptr_t)p.u | (uintptr_t)d_out | (uintptr_t)du | (uintptr_t)out, dtype, p);
   auto k = dtype == kF32 ? (silu ? (gated ? launch_backward<float, true, true> : launch_backward<float, true, false>)
                                  : (gated ? launch_backward<float, false, true> : launch_backward<float, false, false>))
                          : (silu ? (gated ? launch_backward<bf16, true, true> : launch_backward<bf16, true, false>)

@@ -76,17 +76,15 @@ __device__ __forceinline__ void saved8_decode(uint2 codes, unsigned byte, float 
   v[7] = d[1] * scale;
 }
 
-// Eight columns of a row from `p` on, of which `n` are there (the others: zero).  whole: p is a 16-byte boundary and all eight are there.
+// Eight columns of a row from `p` on, of which `n` are there (the others: zero): one vector from wherever it
+// starts where all eight are there (4096 rows of 4097, bf16: saved in 11.6 us, with single values 26.5; of 4096 10.8).
 template <typename T>
-__device__ __forceinline__ void load_eight(float (&v)[8], const T* p, int n, bool whole) {
-  constexpr int V = Vec16<T>::N;
-  if (whole) {
+__device__ __forceinline__ void load_eight(float (&v)[8], const T* p, int n) {
+  if (n >= 8) {
+    T x[8];
+    __builtin_memcpy(x, p, sizeof(x));
 #pragma unroll
-    for (int k = 0; k < 8; k += V) {
-      const Vec16<T> x = load16(p + k);
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[k + i] = to_f32(x.v[i]);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(x[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
@@ -103,15 +101,16 @@ __device__ __forceinline__ void store_past(void* p, uint2 v) {
   __builtin_nontemporal_store(u2{v.x, v.y}, reinterpret_cast<u2*>(p));
 }
 template <typename T>
-__device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int n, bool whole) {
+__device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int n) {
   constexpr int V = Vec16<T>::N;
-  if (whole) {
+  if (n >= 8) {
+    typedef unsigned anywhere __attribute__((ext_vector_type(4), aligned(2)));
 #pragma unroll
     for (int k = 0; k < 8; k += V) {
       Vec16<T> x;
 #pragma unroll
       for (int i = 0; i < V; ++i) x.v[i] = from_f32<T>(v[k + i]);
-      store_past(p + k, *reinterpret_cast<const uint4*>(&x));
+      __builtin_nontemporal_store(__builtin_bit_cast(anywhere, x), reinterpret_cast<anywhere*>(p + k));
     }
   } else {
 #pragma unroll

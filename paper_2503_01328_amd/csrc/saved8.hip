@@ -16,7 +16,6 @@ struct Tensor8 {
   uint32_t chunks;         // eights of codes altogether
   uint32_t row_chunks;     // eights of codes in a row
   int cols;                // of x in a row
-  int vec;                 // rows of x start on 16-byte boundaries
   int flat;                // x is one run of whole blocks: a row of any length
   uint32_t first_block;
 };
@@ -52,7 +51,7 @@ __global__ __launch_bounds__(256) void saved8_kernel(Table8 tab) {
         held[u] = t.cols - (int)col;
       }
       if (SAVE) {
-        load_eight(v[u], at[u], held[u], t.vec && held[u] >= 8);
+        load_eight(v[u], at[u], held[u]);
       } else {
         codes[u] = *(const uint2*)(t.codes + (size_t)i * 8);
         byte[u] = t.scales[i / 4];
@@ -73,7 +72,7 @@ __global__ __launch_bounds__(256) void saved8_kernel(Table8 tab) {
       }
     } else if (i < t.chunks) {
       saved8_decode(codes[u], byte[u], v[u]);
-      store_eight(at[u], v[u], held[u], t.vec && held[u] >= 8);
+      store_eight(at[u], v[u], held[u]);
     }
   }
 }
@@ -136,7 +135,6 @@ bool table_of(const char* what, bool save, int dtype, int n, const void* const* 
     t.cols = cols[i];
     t.chunks = (uint32_t)(saved8_codes(rows[i], cols[i]) / 8);
     t.row_chunks = (uint32_t)(padded / 8);
-    t.vec = (uintptr_t)x[i] % 16 == 0 && (rows[i] == 1 || (int64_t)ld[i] * size % 16 == 0);
     t.flat = padded == cols[i] && (rows[i] == 1 || ld[i] == cols[i]);
     t.first_block = (uint32_t)block;
     block += ceil_div64(t.chunks, 256 * unroll);
