@@ -184,6 +184,7 @@ struct Range {
   int align;
   bool written;
   const void* may_be;
+  bool rows = false;  // an input [rows, h] of dtype: a row is read before any of it is written, as a parameter, which every row reads anew, is not
 };
 bool check_ranges(const char* what, const Range* r, int n) {
   for (int i = 0; i < n; ++i) {
@@ -193,7 +194,7 @@ bool check_ranges(const char* what, const Range* r, int n) {
     }
     for (int j = 0; j < n; ++j) {
       if (i == j || !r[i].written || !overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes)) continue;
-      if (!r[j].written && r[i].p == r[j].p && r[i].bytes == r[j].bytes && r[i].may_be == r[j].p) continue;  // (not a vector that is its first row)
+      if (r[j].rows && r[i].p == r[j].p && r[i].may_be == r[j].p) continue;
       set_error("%s: %s is written and overlaps %s", what, r[i].name, r[j].name);
       return false;
     }
@@ -226,8 +227,8 @@ bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* 
   const uint64_t one = (uint64_t)a.rows * a.h * size, row = (uint64_t)a.h * size, saved = saved8_bytes(a.rows, a.h);
   const Range ranges[] = {{"y", y, one, size, true, x},           {"n", n, one, size, true, f},
                           {"saved_f", saved_f, saved, 16, true, nullptr}, {"saved_y", saved_y, saved, 16, true, nullptr},
-                          {"x", x, one, size, false, nullptr},     {"f", f, one, size, false, nullptr},
-                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr}, {"pre_gain", a.pre_gain, row, size, false, nullptr},
+                          {"x", x, one, size, false, nullptr, true}, {"f", f, one, size, false, nullptr, true},
+                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr, a.gate_per_value != 0}, {"pre_gain", a.pre_gain, row, size, false, nullptr},
                           {"pre_shift", a.pre_shift, row, size, false, nullptr}, {"post_gain", a.post_gain, row, size, false, nullptr},
                           {"post_shift", a.post_shift, row, size, false, nullptr}};
   if (!check_ranges(what, ranges, sizeof(ranges) / sizeof(ranges[0]))) return false;
@@ -292,11 +293,11 @@ bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b,
                           {"dpost_shift", b.dpost_shift, sum, 4, true, nullptr},
                           {"n", b.n, one, size, true, nullptr},
                           {"workspace", b.workspace, norm_join_backward_workspace(a.rows, a.h), 16, true, nullptr},
-                          {"dy", b.dy, one, size, false, nullptr},
-                          {"dn", b.dn, one, size, false, nullptr},
-                          {"y", pre ? b.y : nullptr, b.y_saved8 ? saved : one, b.y_saved8 ? 16 : size, false, nullptr},
-                          {"f", post || gate ? b.f : nullptr, b.f_saved8 ? saved : one, b.f_saved8 ? 16 : size, false, nullptr},
-                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr},
+                          {"dy", b.dy, one, size, false, nullptr, true},
+                          {"dn", b.dn, one, size, false, nullptr, true},
+                          {"y", pre ? b.y : nullptr, b.y_saved8 ? saved : one, b.y_saved8 ? 16 : size, false, nullptr, !b.y_saved8},
+                          {"f", post || gate ? b.f : nullptr, b.f_saved8 ? saved : one, b.f_saved8 ? 16 : size, false, nullptr, !b.f_saved8},
+                          {"gate", a.gate, a.gate_per_value ? one : row, size, false, nullptr, a.gate_per_value != 0},
                           {"pre_gain", a.pre_gain, row, size, false, nullptr},
                           {"pre_shift", a.pre_shift, row, size, false, nullptr},
                           {"post_gain", a.post_gain, row, size, false, nullptr},

@@ -133,6 +133,18 @@ def test_join_backward_refuses(bad):
     _refused("dtype" if "dtype" in bad else "norm_join_backward", po.po_op_norm_join_backward, **{**BACK, **bad})
 
 
+PARAMETERS = ["post_gain", "post_shift", "gate", "pre_gain", "pre_shift"]
+
+
+@pytest.mark.parametrize("name", PARAMETERS)
+def test_join_of_one_row_refuses_parameters_that_are_the_row_it_writes(name):
+    """One row of a tensor is as long as a vector of parameters, which is no tensor that may be overwritten."""
+    for bad in (dict(y=at(0)), dict(n=at(1))):
+        _refused("is written and overlaps " + name, po.po_op_norm_join_forward, **{**JOIN, "rows": 1, **bad, name: at(0) if "y" in bad else at(1)})
+    for bad in (dict(dx=at(0)), dict(df=at(1))):
+        _refused("is written and overlaps " + name, po.po_op_norm_join_backward, **{**BACK, "rows": 1, **bad, name: at(0) if "dx" in bad else at(1)})
+
+
 WEIGHT = dict(dtype=po.PO_BF16, saved_x=at(0), dy=at(2), ldy=24, dw=at(4), ldc=24, accumulate=0, workspace=at(6), rows=4, k=40, n=24)
 
 
