@@ -433,6 +433,26 @@ def test_join_values_that_are_not_finite_stay_in_their_row(gpu_device, rms, post
     assert not got["dx"][bad].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("gate", ["none", "columns"])
+@pytest.mark.parametrize("h", [1, 37, 40, 300, 8200])
+def test_join_checkpoints_of_rows_that_are_not_finite_end_in_zeros(gpu_device, dtype, rms, gate, h):
+    """Rows whose norm is nowhere finite: what lies behind the last column is po_op_save8's zeros, in f's checkpoint and in y's."""
+    dev, (code, tdt), rows = gpu_device, DT[dtype], 6
+    p = dict(_params(dev, tdt, h, rows, rms, True, gate), eps=0.0)
+    x, f = _rand(dev, 75, rows, h, dtype=tdt), _rand(dev, 76, rows, h, dtype=tdt)
+    f[1, h // 2], f[2, h - 1], f[3, 0] = math.nan, math.inf, -math.inf
+    f[4] = 0.0  # a variance of zero, and no eps
+    y, n, sf, sy = _join_forward(dev, dtype, x, f, p)
+    assert y[4].isnan().all() and n[4].isnan().all()
+    for t, s in ((f, sf), (y, sy)):
+        codes, scales = ref.encode(t)
+        got = [v.cpu() for v in ref.split(s, rows, h)]
+        nan = (codes & 127) == 127
+        assert torch.equal((got[0] & 127) == 127, nan) and torch.equal(got[0][~nan], codes[~nan]) and torch.equal(got[1], scales)
+
+
 @pytest.mark.parametrize("rms", [False, True])
 def test_join_of_rows_that_hold_one_value(gpu_device, rms):
     """Variances of zero (LayerNorm of constant rows, rows of zeros), and small and large rows."""
