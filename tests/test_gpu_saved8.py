@@ -544,6 +544,32 @@ def test_weight_grad_of_columns_of_wider_tensors(gpu_device, dtype, rows, k, n, 
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k,n,off", [(16384, 64, 64, 0), (16384, 64, 64, 1), (5000, 65, 77, 1), (700, 100, 120, 0), (700, 100, 120, 3), (3000, 136, 2048, 1),
+                                          (2391, 136, 6368, 0), (3414, 7120, 528, 0)])
+def test_weight_grad_of_columns_of_wider_tensors_in_splits(gpu_device, dtype, rows, k, n, off):
+    """Sums over splits of dy and dw with row strides: more than eight of them, fewer, of small, of middle (fp32) and of wide tiles; whole numbers, exactly, made
+    and added to; what lies beside dy is NaN, what lies beside dw is left alone."""
+    dev, tdt = gpu_device, DT[dtype][1]
+    g = _gen(dev, 140)
+    x = torch.randint(-8, 9, (rows, k), generator=g, device=dev).to(tdt)
+    values = torch.randint(-100, 101, (rows, n), generator=g, device=dev).to(tdt)
+    wide = torch.full((rows + 2, n + 24), math.nan, dtype=tdt, device=dev)
+    dy = wide[1:rows + 1, 8 + off:8 + off + n]
+    dy.copy_(values)
+    saved = _saved(x)
+    want = x.double().T @ values.double()
+    field = torch.full((k + 2, n + 24), MARK, device=dev)
+    dw = field[1:k + 1, 4 + off:4 + off + n]
+    dw.fill_(math.nan)
+    _weight_grad(dtype, saved, dy, dw, 0, k)
+    assert torch.equal(dw.double(), want)
+    _weight_grad(dtype, saved, dy, dw, 1, k)
+    assert torch.equal(dw.double(), 2 * want)
+    dw.fill_(MARK)
+    assert bool((field == MARK).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_weight_grad_workspace_kept_from_more_rows(gpu_device, dtype):
     dev, tdt, k, n = gpu_device, DT[dtype][1], 192, 80
     code = DT[dtype][0]
