@@ -1,8 +1,8 @@
 // A weight's gradient from the 8-bit checkpoint of its input:  dW [k, n] (+)= X^T dY,  X [rows, k] restored (saved8.h), dY [rows, n].
 //
 // A restored value is exact in bf16, so that the product belongs on the bf16 matrix cores whatever type dY has: in bf16 as it is, in
-// fp32 as the sum of three bf16 terms (8 + 8 + 8 significant bits, cut off rather than rounded, which makes the sum exact down to 2^-126), three products of
-// exact operands with fp32 accumulators.  X never exists in 16 bits outside LDS.
+// fp32 as the sum of three bf16 terms (8 + 8 + 8 significant bits, cut off rather than rounded; bits under 2^-133, bf16's smallest number, are lost, so that the
+// sum is exact for magnitudes from 2^-110 on), three products of exact operands with fp32 accumulators; the matrix cores take subnormal terms as they are.  X never exists in 16 bits outside LDS.
 //
 // The contraction is over rows, the slow index of both operands: slices of 64 rows go through registers into LDS as [64][columns] bf16 (codes are
 // scaled on the way: a row's neighbouring columns have one scale), and the fragments come out of it by transposing reads.

@@ -569,6 +569,25 @@ def test_weight_grad_of_columns_of_wider_tensors_in_splits(gpu_device, dtype, ro
     assert bool((field == MARK).all())
 
 
+@pytest.mark.parametrize("rows,k,n", [(1, 40, 24), (2, 2048, 2048), (1, 96, 33)])
+@pytest.mark.parametrize("exponent", [-100, -105, -109, -118, -126])
+def test_weight_grad_of_small_gradients(gpu_device, rows, k, n, exponent):
+    """fp32 dy whose lower bf16 terms are under the normal numbers, and X large enough for a lost one to show: every bit of it down to 2^-110, below that all but
+    what is under 2^-133."""
+    dev = gpu_device
+    bits = torch.randint(0, 1 << 23, (rows, n), generator=_gen(dev, 141), device=dev, dtype=torch.int32)
+    dy = (bits | ((exponent + 127) << 23)).view(torch.float32)
+    dy[:, ::2] *= -1
+    saved = _saved(_rand(dev, 142, rows, k) * 2.0 ** 60)
+    x = ref.stored(saved, rows, k)
+    dw = torch.empty(k, n, device=dev)
+    _weight_grad("f32", saved, dy, dw, 0, k)
+    want = ref.weight_grad(x, dy)
+    if exponent < -110:
+        want = ref.Near(want.v, want.e + x.abs().sum(0)[:, None] * 2.0 ** -133)
+    ref.check(dw, want, "dw")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_weight_grad_workspace_kept_from_more_rows(gpu_device, dtype):
     dev, tdt, k, n = gpu_device, DT[dtype][1], 192, 80
