@@ -432,7 +432,7 @@ int po_op_activation_backward(int32_t dtype, int32_t act, int32_t gated, const v
  * N, a po_norm for both: (v - mean) / sqrt(var + eps) over a row, biased variance, or v / sqrt(mean(v^2) + eps), which has no shifts.  Gains and
  * shifts [h] of dtype, a shift may be NULL.  gate of dtype: [h] (gate_per_value 0) or [rows, h] (1).  saved_f, saved_y: NULL, or the checkpoints of f and
  * of y as it is stored.  y may be x, n may be f; what is written overlaps nothing else.  h 1 to 16384, 1 to 2^25 rows, checkpoints of
- * 2^31 values at most.
+ * 2^31 values at most; the forward fewer than 2^26 waves, of which a row takes one for every 1024 columns begun (over 8192 columns: every 2048).
  * With post_gain and gate NULL and scales of 1 this is a layer's residual sum and LayerNorm. */
 typedef enum { PO_NORM_LAYER = 0, PO_NORM_RMS = 1 } po_norm;
 int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const void* f, const void* post_gain, const void* post_shift,

@@ -163,15 +163,15 @@ __global__ __launch_bounds__(1024) void norm_join_sum_kernel(const float* __rest
 
 int forward_chunks(int h) { return h <= 64 * 8 ? 1 : h <= kMaxWaves * 64 * 8 * 2 ? 2 : 4; }
 
-// saved: whether a checkpoint is read or written.
-bool check(const char* what, int norm, int rows, int h, bool saved, float skip, float branch, float eps) {
+// row_waves: waves of a launch for each row, none where blocks take rows one after another; saved: whether a checkpoint is read or written.
+bool check(const char* what, int norm, int rows, int h, int row_waves, bool saved, float skip, float branch, float eps) {
   if ((norm != kNormLayer && norm != kNormRms) || rows < 1 || rows > kMaxRows || h < 1 || h > kMaxWidth || !(fabsf(skip) < 3e38f) ||
       !(fabsf(branch) < 3e38f) || !(eps >= 0.f) || eps > 3e38f) {
     set_error("%s: norm=%d rows=%d h=%d skip=%g branch=%g eps=%g (norm 0 or 1, 1 to %d rows, h 1 to %d, scales finite, eps finite and not "
               "negative)", what, norm, rows, h, skip, branch, eps, kMaxRows, kMaxWidth);
     return false;
   }
-  if ((int64_t)rows * 64 * waves_of(h, forward_chunks(h)) > UINT32_MAX || (saved && saved8_codes(rows, h) / 8 > kMaxSaved8Chunks)) {
+  if ((int64_t)rows * 64 * row_waves > UINT32_MAX || (saved && saved8_codes(rows, h) / 8 > kMaxSaved8Chunks)) {
     set_error("%s: rows=%d h=%d are too many for a launch, or for a checkpoint (%lld values)", what, rows, h, (long long)kMaxSaved8Chunks * 8);
     return false;
   }
@@ -216,7 +216,7 @@ void launch_forward(const Join& p, hipStream_t stream) {
 bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* f, void* y, void* n, void* saved_f, void* saved_y,
                        hipStream_t stream) {
   const char* what = "norm_join_forward";
-  if (!check(what, a.norm, a.rows, a.h, saved_f || saved_y, a.skip, a.branch, a.eps)) return false;
+  if (!check(what, a.norm, a.rows, a.h, waves_of(a.h, forward_chunks(a.h)), saved_f || saved_y, a.skip, a.branch, a.eps)) return false;
   if (!x || !f || !y || (a.pre_gain == nullptr) != (n == nullptr) || (!a.pre_gain && a.pre_shift) || (!a.post_gain && a.post_shift) ||
       (a.norm == kNormRms && (a.pre_shift || a.post_shift)) || (a.gate_per_value != 0 && a.gate_per_value != 1)) {
     set_error("%s: x=%p f=%p y=%p n=%p pre_gain=%p pre_shift=%p post_gain=%p post_shift=%p gate_per_value=%d (x, f and y given, n with "
@@ -265,7 +265,7 @@ size_t norm_join_backward_workspace(int rows, int h) { return (size_t)blocks_of(
 
 bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream) {
   const char* what = "norm_join_backward";
-  if (!check(what, a.norm, a.rows, a.h, (b.dn && b.y_saved8) || ((a.post_gain || a.gate) && b.f_saved8), a.skip, a.branch, a.eps)) return false;
+  if (!check(what, a.norm, a.rows, a.h, 0, (b.dn && b.y_saved8) || ((a.post_gain || a.gate) && b.f_saved8), a.skip, a.branch, a.eps)) return false;
   const bool pre = b.dn != nullptr, post = a.post_gain != nullptr, gate = a.gate != nullptr, rms = a.norm == kNormRms;
   if (!b.dx || !b.df || (!b.dy && !pre) || pre != (a.pre_gain != nullptr) || (pre && !b.y) || ((post || gate) && !b.f) || (b.n && !pre) ||
       (a.gate_per_value != 0 && a.gate_per_value != 1) || (!pre && a.pre_shift) || (!post && a.post_shift) ||

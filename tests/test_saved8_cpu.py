@@ -133,6 +133,16 @@ def test_join_backward_refuses(bad):
     _refused("dtype" if "dtype" in bad else "norm_join_backward", po.po_op_norm_join_backward, **{**BACK, **bad})
 
 
+@pytest.mark.parametrize("rows,h,forward", [(1 << 25, 1024, True), (1 << 25, 1025, False), ((1 << 25) - 1, 2048, True), (1 << 24, 4096, False), (1 << 23, 8192, False),
+                                            ((1 << 23) - 1, 8192, True), (13421772, 8200, True), (13421773, 8200, False), (1 << 23, 16384, False)])
+def test_join_takes_as_many_rows_as_the_header_says(rows, h, forward):
+    """A forward launches a block a row and no more waves than a launch holds; a backward's blocks take rows one after another, 2^25 of any width.  (What is
+    accepted is refused for a pointer that is missing, so that nothing is launched.)"""
+    _refused("x, f and y given" if forward else "too many for a launch", po.po_op_norm_join_forward,
+             **{**JOIN, "rows": rows, "h": h, "saved_f": None, "saved_y": None, "x": None})
+    _refused("dx, df and dy or dn given", po.po_op_norm_join_backward, **{**BACK, "rows": rows, "h": h, "y_saved8": 0, "f_saved8": 0, "dx": None})
+
+
 PARAMETERS = ["post_gain", "post_shift", "gate", "pre_gain", "pre_shift"]
 
 
