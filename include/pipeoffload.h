@@ -443,8 +443,8 @@ int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const vo
  * will do).  A gradient for every parameter that is given and no other: dpost_gain, dpost_shift, dpre_gain, dpre_shift fp32 [h] +=, in a fixed
  * order; dgate fp32 [h] += for a gate [h], of dtype [rows, h] for one per value.  n: NULL, or n again from y, which the gradient of the weight
  * behind needs.  dx may be dy, df may be dn; what is written overlaps nothing else.  workspace: 16-byte aligned,
- * po_op_norm_join_backward_workspace bytes, contents unspecified before and afterwards; one for more rows (of the same h) serves fewer; NULL where
- * no sum is wanted. */
+ * po_op_norm_join_backward_workspace bytes (0 for a shape that is refused), contents unspecified before and afterwards; one for more rows (of the same
+ * h) serves fewer; NULL where no sum is wanted. */
 uint64_t po_op_norm_join_backward_workspace(int32_t rows, int32_t h);
 int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const void* dn, const void* y, int32_t y_saved8, const void* f,
                              int32_t f_saved8, const void* post_gain, const void* post_shift, const void* gate, int32_t gate_per_value,

@@ -261,7 +261,10 @@ bool norm_join_forward(int dtype, const NormJoin& a, const void* x, const void* 
   return launch_ok("norm_join_forward_kernel");
 }
 
-size_t norm_join_backward_workspace(int rows, int h) { return (size_t)blocks_of(rows, h) * kSums * h * sizeof(float); }
+size_t norm_join_backward_workspace(int rows, int h) {
+  if (rows < 1 || rows > kMaxRows || h < 1 || h > kMaxWidth) return 0;
+  return (size_t)blocks_of(rows, h) * kSums * h * sizeof(float);
+}
 
 bool norm_join_backward(int dtype, const NormJoin& a, const NormJoinBackward& b, hipStream_t stream) {
   const char* what = "norm_join_backward";

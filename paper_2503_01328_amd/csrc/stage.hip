@@ -2007,7 +2007,7 @@ int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const vo
   return ok(norm_join_forward(dtype, a, x, f, y, n, saved_f, saved_y, (hipStream_t)stream));
 }
 uint64_t po_op_norm_join_backward_workspace(int32_t rows, int32_t h) {
-  return rows > 0 && h > 0 ? norm_join_backward_workspace(rows, h) : 0;
+  return norm_join_backward_workspace(rows, h);
 }
 int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const void* dn, const void* y, int32_t y_saved8, const void* f,
                              int32_t f_saved8, const void* post_gain, const void* post_shift, const void* gate, int32_t gate_per_value,

@@ -48,6 +48,12 @@ def test_workspaces_serve_fewer_rows():
     assert po.po_op_weight_grad_saved8_workspace(po.PO_BF16, 64, (1 << 20) + 1, 64) == 0
 
 
+def test_join_workspace_of_shapes_that_are_refused_is_none():
+    assert po.po_op_norm_join_backward_workspace(4, 16385) == po.po_op_norm_join_backward_workspace((1 << 25) + 1, 64) == 0
+    assert po.po_op_norm_join_backward_workspace(4, 2 ** 31 - 1) == po.po_op_norm_join_backward_workspace(-1, 64) == 0
+    assert po.po_op_norm_join_backward_workspace(4, 16384) > 0 and po.po_op_norm_join_backward_workspace(1 << 25, 64) > 0
+
+
 # ---- refusals -----------------------------------------------------------------------------------------------------
 BAD_TENSORS = [[(None, 4, 8, 8)], [(AT, 0, 8, 8)], [(AT, 4, 0, 8)], [(AT, 4, 8, 7)], [(AT + 1, 4, 8, 8)], [(AT, 65537, 32768, 32768)], []]
 
