@@ -439,7 +439,7 @@ int po_op_norm_join_forward(int32_t dtype, int32_t norm, const void* x, const vo
                             const void* gate, int32_t gate_per_value, float skip, float branch, const void* pre_gain, const void* pre_shift,
                             void* y, void* n, void* saved_f, void* saved_y, int32_t rows, int32_t h, float eps, void* stream);
 /* dx and df [rows, h], the gradients of x and f, from dy and dn, those of y and n (dy may be NULL for none; dn NULL: no norm of y, pre_gain NULL too).
- * y and f: checkpoints (y_saved8, f_saved8 not 0) or tensors of dtype; y is read where dn is given, f where post_gain or gate is (else NULL
+ * y and f: checkpoints (y_saved8, f_saved8 not 0) or tensors of dtype (fastest where both are the one or both the other); y is read where dn is given, f where post_gain or gate is (else NULL
  * will do).  A gradient for every parameter that is given and no other: dpost_gain, dpost_shift, dpre_gain, dpre_shift fp32 [h] +=, in a fixed
  * order; dgate fp32 [h] += for a gate [h], of dtype [rows, h] for one per value.  n: NULL, or n again from y, which the gradient of the weight
  * behind needs.  dx may be dy, df may be dn; what is written overlaps nothing else.  workspace: 16-byte aligned,

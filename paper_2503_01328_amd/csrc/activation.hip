@@ -9,7 +9,8 @@
 // Bound by memory: forward u in, out and u's checkpoint out, backward the checkpoint and d in, du and out out.  A lane takes eight columns
 // (gated: eight of a and eight of b), four lanes a block of the checkpoint.  Gated columns that are no whole blocks (f not a multiple of
 // 32: b's blocks begin inside eights of a) go a value at a time, behind a launch that makes the checkpoint.
-// bf16, 4096 rows of 2 x 8192, SiLU: forward 55 us, backward 60 (5.2 to 5.9 TB/s); 128 rows of 1024, fp32: 3.0 and 3.1.
+// bf16, 4096 rows of 2 x 8192, SiLU: forward 55 us (4.9 TB/s), backward 60 (5.6); 128 rows of 1024, fp32: 3.0 and 3.1.  A value at a time, 2 x 8200: forward 86
+// (3.1), backward 165 (2.1), bound by instructions: a division and an access for every value.
 #include <algorithm>
 
 #include "saved8.h"

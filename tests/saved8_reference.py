@@ -3,7 +3,8 @@
 The bounds are a running error analysis: Near carries a value in 64 bits and how far a result computed in fp32 by the same formula can be from it.
 u = 2^-24 is the largest relative error of one rounding to fp32; an operation adds one, and passes its operands' errors on by its derivative.  A
 sum of N terms in any order is off by at most depth u times the sum of their magnitudes, depth the longest chain of additions that a term goes
-through: in a row's sums eight or sixteen in a lane, six over the wave, sixteen over the waves, so that 40 covers them.  Hardware exp2, rcp and rsq are good to 1 ulp
+through: in a row's sums up to 31 in a lane (32 values, the first of which is added to a zero), six over the wave, three over eight waves (the other eight of sixteen
+places hold zeros), or 15, six and four over sixteen, so that 40 covers them.  Hardware exp2, rcp and rsq are good to 1 ulp
 (2 u).  A result rounded to bf16 is off by half a step more, 2^-8 of it at most relative to the power of two below: torch.finfo(t).eps / 2."""
 import math
 
