@@ -454,8 +454,8 @@ int po_op_norm_join_backward(int32_t dtype, int32_t norm, const void* dy, const 
 
 /* A weight's gradient from the checkpoint of its input: dw [k, n] fp32 (row stride ldc) = X^T dY (accumulate 0) or += (1), X [rows, k] as saved_x holds it,
  * dy [rows, n] of dtype (row stride ldy).  Exact products (an fp32 dy's bits under 2^-133 count as zero: values from 2^-110 on are taken whole), fp32 sums, in
- * an order that depends on the sizes, the row strides, dtype and whether dy and dw lie on 16-byte boundaries, on nothing else.  dw overlaps neither input.  workspace: po_op_weight_grad_saved8_workspace bytes (often 0: NULL will do), 16-byte aligned, contents unspecified before and
- * afterwards; one for more rows (of the same dtype, k and n) serves fewer.  1 to 2^25 rows, k and n 1 to 2^20, at most 2^21
+ * an order that depends on the sizes, the row strides, dtype and whether dy and dw lie on 16-byte boundaries, on nothing else.  dw overlaps neither input.
+ * workspace: po_op_weight_grad_saved8_workspace bytes (often 0: NULL will do), 16-byte aligned, contents unspecified before and afterwards; one for more rows (of the same dtype, k and n) serves fewer.  1 to 2^25 rows, k and n 1 to 2^20, at most 2^21
  * tiles of 128 x 128 and 2^31 values of X (beyond: PO_E_INVAL, and 0 bytes), ldy at most 2^22. */
 uint64_t po_op_weight_grad_saved8_workspace(int32_t dtype, int32_t rows, int32_t k, int32_t n);
 int po_op_weight_grad_saved8(int32_t dtype, const void* saved_x, const void* dy, int32_t ldy, float* dw, int32_t ldc, int32_t accumulate,
